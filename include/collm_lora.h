@@ -458,6 +458,106 @@ int collm_adapter_fedavg(int device, collm_dtype dtype, int32_t n_copies, const 
 int collm_adapter_adamw(int device, collm_dtype dtype, void *param, float *master, const float *grad,
                         float *m, float *v, int64_t n_elems, const collm_adamw *hp, void *stream);
 
+/*
+ * What a mixed batch ends in: rows of logits over a vocabulary.  Rows of inference tokens become tokens (collm_sample);
+ * rows of training tokens become a loss against a teacher and the gradient that enters the first backward call
+ * (collm_distill_*); a teacher's rows become the record that the loss reads (collm_top_logits).  The three need no context;
+ * `device` is made current; all are asynchronous on `stream`, may be recorded into a HIP graph, allocate nothing and give the
+ * same bits on every run.
+ *
+ *   logits       dev, element type `dtype`: row r is the `vocab` elements from r * ld on (ld >= vocab), n_held rows in all;
+ *                element-aligned, as is every other pointer of these calls but `workspace`
+ *   rows         dev int32 [n_rows]: row i of the call is row rows[i] of the logits (the rows of the kind in question among
+ *                those of a mixed batch), or NULL: rows 0 .. n_rows - 1 (n_rows <= n_held).  An entry outside
+ *                [0, n_held) is a row that is not there: token -1, an empty record, loss 0.  Where gradients are
+ *                written the entries must differ from each other.
+ *   workspace    dev, 16-byte aligned, workspace_bytes long, contents free, or NULL (0 bytes): calls of few rows cut each row into
+ *                parts and keep the parts' results there; where it does not suffice (COLLM_VOCAB_WORKSPACE bytes always do)
+ *                they take a row at a time, which is slower.  Calls that overlap in time need workspaces of their own.
+ * Limits: 1 <= vocab <= 1048576; COLLM_E_SHAPE otherwise.
+ */
+#define COLLM_VOCAB_WORKSPACE (16 << 20)
+#define COLLM_MAX_TOP 1024      /* entries of a teacher's record of a row */
+#define COLLM_DISTILL_STATS 8   /* floats that collm_distill_fwd keeps of a row */
+typedef struct {
+    int32_t n_rows, n_held, vocab;
+    int32_t dtype;       /* collm_dtype of the logits and of their gradient */
+    int64_t ld;
+    const int32_t *rows; /* dev or NULL */
+} collm_logits;
+
+/*
+ * One token for each row, drawn with the given random number.  The order of a row: falling logits, the lowest index first
+ * among equal ones; what is kept is a beginning of it.  With weights w_v = exp((z_v - max z) / temperature):
+ *   top_k   the first k are kept (k <= 0: off);
+ *   top_p   of those, a token while the weights before it are less than top_p times the sum of theirs; the first always
+ *           (top_p >= 1 or NaN: off);
+ *   min_p   of those, a token whose weight is at least min_p (min_p <= 0 or NaN: off; above 1: 1).
+ * token = the first, in the order, whose running sum of weights exceeds u times the sum of the kept; temperature <= 0 or NaN:
+ * the first in the order.  Weights are computed in 64 bits and added as whole multiples of 2^-45 (less from vocabularies of
+ * 2^17 on).  NaN counts as -inf; a logit of -inf is never kept; where there is +inf, those logits alone weigh, alike.
+ *   params       the rows' parameters, each dev [n_rows] or NULL (temperature 1, the others off); or NULL
+ *   u            dev fp32 [n_rows], each in [0, 1)
+ *   token        dev int32 [n_rows]; -1 where every logit is -inf
+ *   logprob      dev fp32 [n_rows] or NULL: logarithm of the probability, among the kept, of the token (-inf beside token -1)
+ */
+typedef struct {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+} collm_sampling;
+int collm_sample(int device, const collm_logits *shape, const void *logits, const float *u, const collm_sampling *params, int32_t *token,
+                 float *logprob, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * The k largest logits of each row in the order above, and log sum_v exp(z_v / temperature).
+ *   values       dev fp32 [n_rows, k];  indices: dev int32 [n_rows, k].  Where a row has fewer than k logits above -inf:
+ *                -inf and index -1 behind them.  NaN counts as -inf here.
+ *   lse          dev fp32 [n_rows] or NULL; over all logits of the row (a NaN among them: NaN)
+ * 1 <= k <= COLLM_MAX_TOP; temperature > 0 and finite.
+ */
+int collm_top_logits(int device, const collm_logits *shape, const void *logits, int32_t k, float temperature, float *values, int32_t *indices,
+                     float *lse, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Distillation from a teacher's top logits.  With the student's logits z of a row, q = softmax(z / tau), the record's k logits t
+ * and places:
+ *   lse == NULL: p = softmax(t / tau), r = 0;
+ *   lse given:   p = exp(t / tau - lse), the teacher's own probabilities (lse as collm_top_logits gives it at the same
+ *                temperature), and r = max(0, 1 - sum p) for all places outside the record;
+ *   KD   = sum_k p_k (log p_k - log q at place k) + r (log r - log sum_{outside} q)
+ *   loss = kd_weight tau^2 KD + ce_weight CE,   CE = -log softmax(z)[label]
+ * and its gradient with respect to z, times dloss of the row (P = sum p + r):
+ *   kd_weight tau (P q_v - p_v - [v outside] r q_v / sum_{outside} q) + ce_weight (softmax(z)_v - [v = label]).
+ * An entry of the record whose index is outside [0, vocab) or whose value is -inf is none; a row without any has no KD; p_k = 0
+ * adds nothing; where no logit outside the record is above -inf there is no term of r.  A label outside [0, vocab)
+ * (say -100) is none.  A row whose logits are all -inf has loss 0 and gradient 0.  NaN logits give NaN.
+ *   values       dev fp32 [n_rows, k];  indices: dev int32 [n_rows, k] (a place named twice counts as often);
+ *   lse          dev fp32 [n_rows] or NULL;  labels: dev int32 [n_rows] or NULL
+ *   loss         dev fp32 [n_rows]
+ *   stats        dev fp32 [n_rows, COLLM_DISTILL_STATS]: written by the forward call if not NULL, read by the backward call of
+ *                the same arguments
+ *   dloss        dev fp32 [n_rows]
+ *   dlogits      dev, element type `dtype`, rows as those of the logits with ld_grad elements from one to the next; only the call's
+ *                rows are written.  Either apart from the logits or in their place (same pointer, ld_grad == ld).
+ * Sums are kept in 32 bits within a thread and in 64 across threads; a gradient is rounded once.
+ * 1 <= k <= COLLM_MAX_TOP; temperature > 0; weights finite.  collm_distill_fwd_bwd is both calls in one that reads the logits once.
+ */
+typedef struct {
+    int32_t k;
+    const float *values;
+    const int32_t *indices;
+    const float *lse;
+    const int32_t *labels;
+    float temperature, kd_weight, ce_weight;
+} collm_distill;
+int collm_distill_fwd(int device, const collm_logits *shape, const void *logits, const collm_distill *teacher, float *loss, float *stats,
+                      void *workspace, int64_t workspace_bytes, void *stream);
+int collm_distill_bwd(int device, const collm_logits *shape, const void *logits, const collm_distill *teacher, const float *stats, const float *dloss,
+                      void *dlogits, int64_t ld_grad, void *stream);
+int collm_distill_fwd_bwd(int device, const collm_logits *shape, const void *logits, const collm_distill *teacher, const float *dloss, float *loss,
+                          void *dlogits, int64_t ld_grad, void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -53,6 +53,20 @@ class collm_adamw(ctypes.Structure):
     ]
 
 
+class collm_logits(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int32), ("n_held", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("ld", ctypes.c_int64), ("rows", ctypes.c_void_p)]
+
+
+class collm_sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
+
+
+class collm_distill(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_int32), ("values", ctypes.c_void_p), ("indices", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("labels", ctypes.c_void_p), ("temperature", ctypes.c_float), ("kd_weight", ctypes.c_float), ("ce_weight", ctypes.c_float)]
+
+
 _lib = None
 _marshal = None  # compiled argument marshalling of the compute calls (csrc/marshal.cpp); None: every call by the ctypes route
 _i32p = ctypes.POINTER(ctypes.c_int32)
@@ -154,6 +168,14 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.collm_adapter_adamw.argtypes = [ctypes.c_int, ctypes.c_int, vp, vp, vp, vp, vp, ctypes.c_int64,
                                         ctypes.POINTER(collm_adamw), vp]
     lib.collm_adapter_adamw.restype = ctypes.c_int
+    lp, dp, i64 = ctypes.POINTER(collm_logits), ctypes.POINTER(collm_distill), ctypes.c_int64
+    lib.collm_sample.argtypes = [ctypes.c_int, lp, vp, vp, ctypes.POINTER(collm_sampling), vp, vp, vp, i64, vp]
+    lib.collm_top_logits.argtypes = [ctypes.c_int, lp, vp, i32, ctypes.c_float, vp, vp, vp, vp, i64, vp]
+    lib.collm_distill_fwd.argtypes = [ctypes.c_int, lp, vp, dp, vp, vp, vp, i64, vp]
+    lib.collm_distill_bwd.argtypes = [ctypes.c_int, lp, vp, dp, vp, vp, vp, i64, vp]
+    lib.collm_distill_fwd_bwd.argtypes = [ctypes.c_int, lp, vp, dp, vp, vp, vp, i64, vp, i64, vp]
+    for f in (lib.collm_sample, lib.collm_top_logits, lib.collm_distill_fwd, lib.collm_distill_bwd, lib.collm_distill_fwd_bwd):
+        f.restype = ctypes.c_int
     if torch is not None and os.path.exists(MARSHAL_PATH):
         spec = importlib.util.spec_from_file_location("_marshal", MARSHAL_PATH)
         marshal = importlib.util.module_from_spec(spec)
@@ -598,3 +620,131 @@ def collm_adapter_adamw(param, grad, m, v, lr: float, beta1: float, beta2: float
                                    v.data_ptr(), param.numel(), ctypes.byref(hp), _stream_handle(stream)),
            "collm_adapter_adamw")
     return param
+
+
+# ----------------------------------------------------------------------------------------------------------------------
+# rows of logits
+# ----------------------------------------------------------------------------------------------------------------------
+VOCAB_WORKSPACE = 16 << 20  # bytes of workspace that suffice for every call below
+MAX_TOP = 1024              # entries of a teacher's record of a row
+DISTILL_STATS = 8           # floats that collm_distill_fwd keeps of a row
+
+
+def _data(t, shape, dtype, like, what):
+    """Address of a contiguous tensor of the given shape and type on the device of `like`; None is NULL."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != like.device:
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape} on {like.device}")
+    return t.data_ptr()
+
+
+def _matrix(t, what):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what} must be [rows, vocab] with neighbouring columns side by side")
+    return max(int(t.stride(0)), int(t.shape[1])) if t.shape[0] <= 1 else int(t.stride(0))
+
+
+def _logits(logits, n_rows, rows):
+    import torch
+
+    return collm_logits(n_rows, int(logits.shape[0]), int(logits.shape[1]), _dtype_of(logits), _matrix(logits, "logits"),
+                        _data(rows, (n_rows,), torch.int32, logits, "rows"))
+
+
+def _workspace(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def collm_sample(logits, u, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None, rows=None, workspace=None, stream=None):
+    """token[i] (int32) <- the token that u[i] draws from row i of the logits (row rows[i], if `rows` is given) under its temperature,
+    top-k, top-p and min-p ([n] tensors; None: 1, off); logprob[i] <- the logarithm of its probability among those kept."""
+    import torch
+
+    lib = load_library()
+    n = int(u.shape[0])
+    sh = _logits(logits, n, rows)
+    f32 = lambda t, what: _data(t, (n,), torch.float32, logits, what)
+    pr = collm_sampling(f32(temperature, "temperature"), _data(top_k, (n,), torch.int32, logits, "top_k"), f32(top_p, "top_p"),
+                        f32(min_p, "min_p"))
+    _check(lib.collm_sample(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), f32(u, "u"), ctypes.byref(pr),
+                            _data(token, (n,), torch.int32, logits, "token"), f32(logprob, "logprob"), *_workspace(workspace),
+                            _stream_handle(stream)), "collm_sample")
+    return token
+
+
+def collm_top_logits(logits, values, indices, lse=None, temperature=1.0, rows=None, workspace=None, stream=None):
+    """values [n, k] (fp32), indices [n, k] (int32) <- the k largest logits of each row, largest first; lse [n] <- log-sum-exp of
+    row / temperature."""
+    import torch
+
+    lib = load_library()
+    n, k = (int(v) for v in values.shape)
+    sh = _logits(logits, n, rows)
+    _check(lib.collm_top_logits(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), k, float(temperature),
+                                _data(values, (n, k), torch.float32, logits, "values"),
+                                _data(indices, (n, k), torch.int32, logits, "indices"), _data(lse, (n,), torch.float32, logits, "lse"),
+                                *_workspace(workspace), _stream_handle(stream)), "collm_top_logits")
+    return values, indices
+
+
+def _teacher(logits, t_values, t_indices, t_lse, labels, temperature, kd_weight, ce_weight):
+    import torch
+
+    n, k = (int(v) for v in t_values.shape)
+    return n, collm_distill(k, _data(t_values, (n, k), torch.float32, logits, "t_values"),
+                            _data(t_indices, (n, k), torch.int32, logits, "t_indices"), _data(t_lse, (n,), torch.float32, logits, "t_lse"),
+                            _data(labels, (n,), torch.int32, logits, "labels"), float(temperature), float(kd_weight), float(ce_weight))
+
+
+def _grad(logits, dlogits):
+    if dlogits.shape != logits.shape or dlogits.dtype != logits.dtype or dlogits.device != logits.device:
+        raise ValueError("dlogits must have the shape, type and device of logits")
+    return dlogits.data_ptr(), _matrix(dlogits, "dlogits")
+
+
+def collm_distill_fwd(logits, t_values, t_indices, loss, stats=None, t_lse=None, labels=None, temperature=1.0, kd_weight=1.0, ce_weight=0.0,
+                      rows=None, workspace=None, stream=None):
+    """loss[i] <- kd_weight tau^2 KL(teacher's record of row i || softmax(row / tau)) + ce_weight cross entropy of its label.
+    The record: t_values, t_indices [n, k] as collm_top_logits gives them, with t_lse the teacher's true probabilities.
+    stats [n, DISTILL_STATS] (optional): what collm_distill_bwd needs."""
+    import torch
+
+    lib = load_library()
+    n, d = _teacher(logits, t_values, t_indices, t_lse, labels, temperature, kd_weight, ce_weight)
+    sh = _logits(logits, n, rows)
+    _check(lib.collm_distill_fwd(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d),
+                                 _data(loss, (n,), torch.float32, logits, "loss"),
+                                 _data(stats, (n, DISTILL_STATS), torch.float32, logits, "stats"), *_workspace(workspace),
+                                 _stream_handle(stream)), "collm_distill_fwd")
+    return loss
+
+
+def collm_distill_bwd(logits, t_values, t_indices, stats, dloss, dlogits, t_lse=None, labels=None, temperature=1.0, kd_weight=1.0,
+                      ce_weight=0.0, rows=None, workspace=None, stream=None):
+    """dlogits (the call's rows; may be `logits` itself) <- dloss[i] times the gradient of row i's loss.  Every other argument as
+    in the forward call that wrote `stats` (workspace is not used)."""
+    import torch
+
+    lib = load_library()
+    n, d = _teacher(logits, t_values, t_indices, t_lse, labels, temperature, kd_weight, ce_weight)
+    sh = _logits(logits, n, rows)
+    _check(lib.collm_distill_bwd(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d),
+                                 _data(stats, (n, DISTILL_STATS), torch.float32, logits, "stats"),
+                                 _data(dloss, (n,), torch.float32, logits, "dloss"), *_grad(logits, dlogits), _stream_handle(stream)),
+           "collm_distill_bwd")
+    return dlogits
+
+
+def collm_distill_fwd_bwd(logits, t_values, t_indices, dloss, loss, dlogits, t_lse=None, labels=None, temperature=1.0, kd_weight=1.0,
+                          ce_weight=0.0, rows=None, workspace=None, stream=None):
+    """Both calls in one that reads the logits once: the loss of each row and dlogits <- dloss[i] times its gradient."""
+    import torch
+
+    lib = load_library()
+    n, d = _teacher(logits, t_values, t_indices, t_lse, labels, temperature, kd_weight, ce_weight)
+    sh = _logits(logits, n, rows)
+    _check(lib.collm_distill_fwd_bwd(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d),
+                                     _data(dloss, (n,), torch.float32, logits, "dloss"), _data(loss, (n,), torch.float32, logits, "loss"),
+                                     *_grad(logits, dlogits), *_workspace(workspace), _stream_handle(stream)), "collm_distill_fwd_bwd")
+    return loss

@@ -15,16 +15,16 @@
 #include "collm_lora.h"
 #include "kernels.h"
 #include "planner.h"
+#include "status.h"
 
 using namespace collm;
 
-namespace collm {
-thread_local LaunchEvents g_launch_events;
+namespace {
+thread_local std::string g_last_error;
 }
 
-namespace {
-
-thread_local std::string g_last_error;
+namespace collm {
+thread_local LaunchEvents g_launch_events;
 
 int hip_fail(hipError_t e, const char *what)
 {
@@ -33,12 +33,9 @@ int hip_fail(hipError_t e, const char *what)
     g_last_error = buf;
     return COLLM_E_HIP;
 }
+}  // namespace collm
 
-#define HIP_TRY(expr)                                     \
-    do {                                                  \
-        hipError_t e_ = (expr);                           \
-        if (e_ != hipSuccess) return hip_fail(e_, #expr); \
-    } while (0)
+namespace {
 
 constexpr int kSlots = 16;             // pinned staging ring: the host may run this many uploads ahead
 constexpr uint64_t kWarmMaxBytes = (uint64_t)40 << 20;  // largest weight a rank-wide pass fetches ahead of its GEMM

@@ -1,0 +1,63 @@
+// Argument blocks and launchers of the vocabulary operators (kernels_sample.hip, kernels_distill.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace collm {
+
+constexpr int kMaxVocab = 1 << 20;  // columns of a row of logits (a bitmap of a row fits the LDS; fixed-point sums have 20 bits to grow)
+constexpr int kMaxTop = 1024;       // entries of a teacher's record
+
+// The rows of one call: row i of the call is row (rows ? rows[i] : i) of the logits; an entry of `rows` outside
+// [0, n_held) is a row that is not there
+struct LogitRows {
+    const void *logits;
+    int64_t ld;
+    const int32_t *rows;
+    int n_rows, n_held, vocab;
+    bool bf16;
+};
+
+struct SampleArgs {
+    LogitRows r;
+    const float *u, *temperature;  // temperature NULL: 1
+    const int32_t *top_k;          // NULL: off
+    const float *top_p, *min_p;    // NULL: off
+    int32_t *token;
+    float *logprob;                // optional
+};
+
+struct TopArgs {
+    LogitRows r;
+    int k;
+    float temperature;
+    float *values;     // [n_rows, k]
+    int32_t *indices;  // [n_rows, k]
+    float *lse;        // optional
+};
+
+// floats that a forward call keeps of a row for the backward call
+constexpr int kDistillStats = 8;
+
+struct DistillArgs {
+    LogitRows r;
+    int k;
+    const float *t_values;    // [n_rows, k]
+    const int32_t *t_indices;
+    const float *t_lse;       // [n_rows] or NULL: the record's probabilities sum to one
+    const int32_t *labels;    // [n_rows] or NULL
+    float temperature, kd_weight, ce_weight;
+    float *loss;              // forward
+    float *stats;             // forward: written if not NULL; backward alone: read
+    const float *dloss;       // gradient
+    void *dlogits;
+    int64_t ld_grad;
+};
+
+hipError_t launch_sample(const SampleArgs &a, hipStream_t st);
+hipError_t launch_top_logits(const TopArgs &a, hipStream_t st);
+hipError_t launch_distill_fwd(const DistillArgs &a, hipStream_t st);
+hipError_t launch_distill_bwd(const DistillArgs &a, hipStream_t st);
+hipError_t launch_distill_fwd_bwd(const DistillArgs &a, hipStream_t st);
+
+}  // namespace collm
