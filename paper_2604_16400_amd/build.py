@@ -25,6 +25,9 @@ FLAGS = [
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 
+# kernels that hold a row in registers through a loop over rows: constants of the loop moved in front of it would take the row's registers
+SOURCE_FLAGS = {"kernels_distill.hip": ["-mllvm", "-disable-machine-licm"]}
+
 
 def _stale(out: str, deps) -> bool:
     if not os.path.exists(out):
@@ -77,7 +80,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs.append(o)
         if force or _stale(o, [s] + hdrs):
             lang = ["-x", "hip"]
-            jobs.append([hipcc] + FLAGS + lang + ["-c", s, "-o", o])
+            jobs.append([hipcc] + FLAGS + SOURCE_FLAGS.get(src, []) + lang + ["-c", s, "-o", o])
 
     with ThreadPoolExecutor(max_workers=4) as ex:
         list(ex.map(lambda cmd: _run(cmd, verbose), jobs))

@@ -140,6 +140,7 @@ int collm_distill_fwd(int device, const collm_logits *shape, const void *logits,
     a.loss = loss;
     a.stats = stats;
     HIP_TRY(hipSetDevice(device));
+    HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
     HIP_TRY(launch_distill_fwd(a, (hipStream_t)stream));
     return COLLM_OK;
 }
@@ -177,6 +178,7 @@ int collm_distill_fwd_bwd(int device, const collm_logits *shape, const void *log
     a.dlogits = dlogits;
     a.ld_grad = ld_grad;
     HIP_TRY(hipSetDevice(device));
+    HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
     HIP_TRY(launch_distill_fwd_bwd(a, (hipStream_t)stream));
     return COLLM_OK;
 }

@@ -122,14 +122,15 @@ template <bool BF16, int THREADS> struct Picker {
 
     __device__ __forceinline__ Picker(Shared<THREADS> &s, const void *p, int vocab) : sh(s), row(p, vocab) {}
 
-    // f(key, index) over the row's logits; elements outside the row come as -inf
+    // f(key, index) over the row's logits
     template <typename F> __device__ __forceinline__ void each(F f) const
     {
-        for (int c = threadIdx.x; c < row.chunks; c += THREADS) {
-            const uint4 v = row.load(c);
+        for (int c = threadIdx.x; c < row.whole; c += THREADS) {
+            const uint4 v = row.body[c];
 #pragma unroll
-            for (int e = 0; e < Row<BF16>::E; ++e) f(key_of(Row<BF16>::value(v, e)), c * Row<BF16>::E - row.head + e);
+            for (int e = 0; e < Row<BF16>::E; ++e) f(key_of(Row<BF16>::value(v, e)), row.lo + c * Row<BF16>::E + e);
         }
+        if ((int)threadIdx.x < row.edges) f(key_of(row.edge(threadIdx.x)), row.edge_index(threadIdx.x));
     }
     __device__ __forceinline__ void clear(u64 *hist) const
     {
@@ -311,9 +312,10 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS) top
     m = block_max<THREADS>(m, sh.red);
     if (p.lse) {
         const float inv = 1.0f / p.temperature, ref = m > kNegInf ? m : 0.0f;
-        float part = 0.f;  // (of the logits as they are: a NaN among them shows)
-        for (int c = threadIdx.x; c < pick.row.chunks; c += THREADS) {
-            const uint4 v = pick.row.load(c);
+        // (of the logits as they are: a NaN among them shows)
+        float part = expf((pick.row.edge(threadIdx.x) - ref) * inv);
+        for (int c = threadIdx.x; c < pick.row.whole; c += THREADS) {
+            const uint4 v = pick.row.body[c];
 #pragma unroll
             for (int e = 0; e < Row<BF16>::E; ++e) part += expf((Row<BF16>::value(v, e) - ref) * inv);
         }

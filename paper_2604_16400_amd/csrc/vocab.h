@@ -52,6 +52,7 @@ struct DistillArgs {
     const float *dloss;       // gradient
     void *dlogits;
     int64_t ld_grad;
+    int compute_units;        // of the GPU
 };
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t st);

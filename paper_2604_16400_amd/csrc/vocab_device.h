@@ -35,41 +35,37 @@ template <> struct Elem<false> {
     static __device__ __forceinline__ void store(void *row, int64_t i, float v) { ((float *)row)[i] = v; }
 };
 
-// A row of logits as the 16-byte chunks of memory that hold it.  Element i of the row is element (i + head) % E of chunk
-// (i + head) / E.  The first and the last chunk may hold only a few elements of the row: those are read one by one, as
-// nothing outside the row may be.
+// A row of logits as the whole 16-byte chunks of memory inside it and the few elements before and behind them, its edges
+// (fewer than a chunk on either side).  Element e of chunk c is element lo + c E + e of the row; edge t, which thread t
+// takes, is element t (t < lo) or whole E + t.
 template <bool BF16> struct Row {
     static constexpr int E = Elem<BF16>::kPerChunk;
-    const void *row;  // first element
-    int n, head, chunks;
+    const void *row;   // first element
+    const uint4 *body; // first whole chunk
+    int n, lo, whole, edges;
 
     __device__ __forceinline__ Row(const void *p, int vocab) : row(p), n(vocab)
     {
-        head = (int)(((uintptr_t)p & 15u) / (16 / E));
-        chunks = (vocab + head + E - 1) / E;
+        const int head = (int)(((uintptr_t)p & 15u) / (16 / E));
+        lo = (E - head) % E;
+        if (lo > n) lo = n;
+        whole = (n - lo) / E;
+        edges = n - whole * E;
+        body = (const uint4 *)((const char *)p + lo * (16 / E));
     }
-    __device__ __forceinline__ const uint4 *base() const { return (const uint4 *)((uintptr_t)row & ~(uintptr_t)15); }
-    __device__ __forceinline__ bool whole(int c) const { return c * E >= head && (c + 1) * E <= n + head; }
-    __device__ __forceinline__ uint4 edge(int c) const  // elements outside the row: -inf
+    // the whole chunks as a buffer: reads beyond them give 0
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const
     {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (BF16) {
-                const int i = c * E - head + 2 * j;
-                uint32_t lo = 0xff80u, hi = 0xff80u;
-                if (i >= 0 && i < n) lo = ((const uint16_t *)row)[i];
-                if (i + 1 >= 0 && i + 1 < n) hi = ((const uint16_t *)row)[i + 1];
-                w[j] = lo | (hi << 16);
-            } else {
-                const int i = c * E - head + j;
-                w[j] = 0xff800000u;
-                if (i >= 0 && i < n) w[j] = ((const uint32_t *)row)[i];
-            }
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+        return __builtin_amdgcn_make_buffer_rsrc((void *)body, 0, whole * 16, 0x00020000);
     }
-    __device__ __forceinline__ uint4 load(int c) const { return whole(c) ? base()[c] : edge(c); }
+    __device__ __forceinline__ int edge_index(int t) const { return t < lo ? t : whole * E + t; }
+    __device__ __forceinline__ float edge(int t) const { return t < edges ? Elem<BF16>::load(row, edge_index(t)) : kNegInf; }
+    // a number for each element: chunk by chunk, then the edges
+    __device__ __forceinline__ int bit(int i) const
+    {
+        if (i < lo) return whole * E + i;
+        return i < lo + whole * E ? i - lo : i;
+    }
     // value of element e of a chunk
     static __device__ __forceinline__ float value(const uint4 &v, int e)
     {
@@ -77,29 +73,44 @@ template <bool BF16> struct Row {
         if (!BF16) return __uint_as_float(w[e]);
         return __uint_as_float((e & 1) ? (w[e >> 1] & 0xffff0000u) : (w[e >> 1] << 16));
     }
+    static __device__ __forceinline__ uint4 chunk(const float (&g)[8])
+    {
+        if (!BF16) return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+        return make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]), pack_bf16(g[6], g[7]));
+    }
 };
 
 // first element of row i of a call; NULL where it is not there
 __device__ __forceinline__ const void *row_of(const LogitRows &r, int i)
 {
-    const int64_t at = r.rows ? (int64_t)r.rows[i] : i;
+    const int64_t at = r.rows ? (int64_t)__builtin_amdgcn_readfirstlane(r.rows[i]) : i;
     if (at < 0 || at >= r.n_held) return nullptr;
     return (const char *)r.logits + at * r.ld * (r.bf16 ? 2 : 4);
 }
 
-// ---- block-wide reductions (every thread gets the result); `s` holds one value a wave and is free again on return ----
+// ---- block-wide reductions (every thread gets the result, in scalar registers); `s` holds one value a wave and is free again on return ----
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+__device__ __forceinline__ unsigned long long uniform(unsigned long long v)
+{
+    return (unsigned long long)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v);
+}
+__device__ __forceinline__ double uniform(double v) { return __longlong_as_double((long long)uniform((unsigned long long)__double_as_longlong(v))); }
+
 template <typename T, int THREADS, typename F> __device__ __forceinline__ T block_reduce(T v, T *s, F f)
 {
+    constexpr int W = THREADS / kWave;
 #pragma unroll
     for (int o = kWave / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o));
-    if (THREADS == kWave) return v;
-    if ((threadIdx.x & (kWave - 1)) == 0) s[threadIdx.x / kWave] = v;
+    if (W == 1) return uniform(v);
+    const int lane = threadIdx.x & (kWave - 1);
+    if (lane == 0) s[threadIdx.x / kWave] = v;
     __syncthreads();
-    T r = s[0];
+    v = s[lane & (W - 1)];
 #pragma unroll
-    for (int w = 1; w < THREADS / kWave; ++w) r = f(r, s[w]);
+    for (int o = W / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o));
     __syncthreads();
-    return r;
+    return uniform(v);
 }
 template <int THREADS> __device__ __forceinline__ float block_max(float v, double *s)
 {

@@ -323,6 +323,46 @@ def test_distill_rows_of_a_batch(how):
     _distill_case(777, "bf16", 12, 1.0, True, True, 5, how, ld=784, ld_grad=784, pick=[3, 0, 16, 9, -1, 7, 12, 15])
 
 
+@pytest.mark.parametrize("how", ["loss", "two", "step", "in place"])
+@pytest.mark.parametrize("dtype,V,n,copies", [("bf16", 257, 16, 130), ("bf16", 40000, 7, 90), ("bf16", 70001, 7, 50), ("f32", 30001, 5, 120)])
+def test_distill_more_rows_than_blocks(dtype, V, n, copies, how):
+    """Blocks that take several rows: copies of a few rows in another order, each row's results those of its first (all rows begin
+    on 16 bytes: a row's sums are taken chunk by chunk)."""
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    k, tau = 20, 2.0
+    z = _distill_rows(V, rng)[:n]
+    values, at, lse = _record(z, k, tau, rng)
+    lab = rng.integers(-1, V, size=n).astype(np.int32)
+    dloss = (rng.random(n) + 0.5).astype(np.float32)
+    order = np.concatenate([np.arange(n)] + [rng.permutation(n) for _ in range(copies - 1)])
+    pick = _up(order, torch.int64)
+    ld = (V + 7) // 8 * 8
+    few = _place(z, dtype, ld)
+    dev = torch.empty((len(order), ld), dtype=few.dtype, device="cuda")[:, :V]
+    dev.copy_(few[pick])
+    host = _back(few)
+    big = lambda x, dt=None: _up(x, dt)[pick].contiguous()
+    m = len(order)
+    loss = torch.full((m,), NAN, device="cuda")
+    stats = torch.full((m, b.DISTILL_STATS), NAN, device="cuda")
+    t = (big(values), big(at, torch.int32))
+    kw = dict(t_lse=big(lse), labels=big(lab, torch.int32), temperature=tau, kd_weight=0.7, ce_weight=0.3)
+    grad = None if how == "loss" else dev if how == "in place" else torch.full((m, ld), 7.5, dtype=dev.dtype, device="cuda")[:, :V]
+    if how == "loss":
+        b.collm_distill_fwd(dev, *t, loss, **kw)
+    elif how == "two":
+        b.collm_distill_fwd(dev, *t, loss, stats, **kw)
+        b.collm_distill_bwd(dev, *t, stats, big(dloss), grad, **kw)
+    else:
+        b.collm_distill_fwd_bwd(dev, *t, big(dloss), loss, grad, **kw)
+    _check_distill(_back(loss[:n]), None if grad is None else _back(grad[:n]), host, values, at, lse, lab, dloss, V, dtype, tau, np.float32(0.7),
+                   np.float32(0.3))
+    assert torch.equal(loss, loss[:n][pick])
+    if grad is not None:
+        assert torch.equal(grad, grad[:n][pick])
+
+
 def test_distill_mass_far_outside_the_record():
     """The rest of the row is so far below the record that 1 - sum q is nothing in 64 bits: its own sum keeps it."""
     torch = _torch()
