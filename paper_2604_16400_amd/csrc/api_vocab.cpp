@@ -159,6 +159,7 @@ int collm_distill_bwd(int device, const collm_logits *shape, const void *logits,
     a.dlogits = dlogits;
     a.ld_grad = ld_grad;
     HIP_TRY(hipSetDevice(device));
+    HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
     HIP_TRY(launch_distill_bwd(a, (hipStream_t)stream));
     return COLLM_OK;
 }

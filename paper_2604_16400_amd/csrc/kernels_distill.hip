@@ -6,11 +6,15 @@
 //   KD   = sum_k p_k (log p_k - log q_k) + r (log r - log sum_rest q)
 //   loss = a tau^2 KD + b CE,   CE = -log softmax(z)[label]
 //   dloss/dz_v = a tau (P q_v - p_v - [v in rest] r q_v / sum_rest q) + b (softmax(z)_v - [v = label]).
-// Outside the record the gradient is one multiple of exp((z_v - ref) / tau) plus one of exp(z_v - max): the row is two
+// Outside the record the gradient is one multiple of exp((z_v - ref) / tau) plus one of exp(z_v - ref): the row is two
 // coefficients, and the places of the record and of the label are written again, behind the others, from sums in 64 bits.
-// The sum over the rest is taken over the rest alone (a bitmap of the record in shared memory masks it), relative to its own
-// largest logit: 1 - sum q would lose it where the record holds nearly all of the mass.  Sums are taken in one pass, each thread
-// relative to the largest logit that it has met.
+// The sum over the rest is taken over the rest alone (a bitmap of the record in shared memory masks it): 1 - sum q would lose it
+// where the record holds nearly all of the mass.
+//
+// The sums need no largest logit first.  They are taken relative to the student's largest logit in the record, which is near the
+// row's where student and teacher agree, so that an exponential is one fused multiply-add and one exp2.  Where a sum then is not
+// finite, or so small that terms may have vanished, the row is summed again, each thread relative to the largest logit that it
+// has met.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -27,22 +31,35 @@ using namespace vocab;
 
 constexpr float kLow = -3.402823466e+38f;  // the least finite value: a running maximum begins here, so that -inf adds nothing
 
-// exp(d / tau) for d <= 0: the rounding of the factor and of the product are errors of |d / tau| 2^-24 each, small where the result is not
+// exp((z - ref) / tau).  near: 2^32 times that (what is below 2^-126 is lost: this is 2^-158 then), as exp2(z c + b) with b = 32 - ref c
+// rounded beforehand: the same factor 2^drift in every term, taken out in 64 bits.  Otherwise (ref too large for that) from the difference.
+// The rounding of c and of the argument are errors of |z - ref| / tau 2^-24 each, small where the result is not.
 struct Exp {
-    float c;
-    __device__ __forceinline__ explicit Exp(float tau) : c(uniform((float)(1.44269504088896340736 / (double)tau))) {}
-    __device__ __forceinline__ float operator()(float d) const { return __builtin_amdgcn_exp2f(d * c); }
+    float c, ref, b;
+    __device__ __forceinline__ Exp(float tau, float r) : c(uniform((float)(1.44269504088896340736 / (double)tau))), ref(r), b(__builtin_fmaf(-r, c, 32.f)) {}
+    __device__ __forceinline__ float near(float z) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, c, b)); }
+    __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z - ref) * c); }
+    __device__ __forceinline__ double drift() const { return (double)ref * (double)c + (double)b; }  // 32, about
 };
 
-// A teacher's record of a row in shared memory, and what the waves of a block tell each other
+// What the waves of a block tell each other, and a teacher's record of a row, in shared memory
 template <int THREADS> struct Shared {
     double sum[THREADS / kWave], sum_ce[THREADS / kWave];
     float max[THREADS / kWave];
-    float coef[8];
-    double p[kMaxTop];       // probabilities (of a place named twice: their sum, at its first entry)
-    float t[kMaxTop], z[kMaxTop];  // the teacher's and the student's logits
-    int32_t at[kMaxTop];     // places; -1: not an entry
-    uint8_t first[kMaxTop];  // whether the entry is its place's first
+    float coef[kDistillStats];
+};
+// (dynamic: k entries of each, the bitmap of the row behind them)
+struct Record {
+    double *p;       // probabilities (of a place named twice: their sum, at its first entry)
+    float *t, *z;    // the teacher's and the student's logits
+    int32_t *at;     // places; -1: not an entry
+    uint32_t *bits;  // one bit an element of the row
+    uint8_t *first;  // whether the entry is its place's first
+    __device__ __forceinline__ Record(double *mem, int k, int vocab)
+        : p(mem), t((float *)(mem + k)), z(t + k), at((int32_t *)(z + k)), bits((uint32_t *)(at + k)), first((uint8_t *)(bits + (vocab + 31) / 32))
+    {
+    }
+    static size_t bytes(int k, int vocab) { return (size_t)k * 21 + ((size_t)vocab + 31) / 32 * 4; }
 };
 
 struct Entry {
@@ -67,7 +84,7 @@ template <bool BF16> __device__ __forceinline__ void load_logit(Entry &e, const 
 
 // Row i's record into shared memory, its places into the bitmap.  mine: the entry of this thread's index, loaded before.
 template <bool BF16, int THREADS>
-__device__ __forceinline__ void put_record(Shared<THREADS> &sh, uint32_t *bits, const DistillArgs &p, int i, const Row<BF16> &row, const Entry &mine)
+__device__ __forceinline__ void put_record(const Record &rec, const DistillArgs &p, int i, const Row<BF16> &row, const Entry &mine)
 {
     for (int j = threadIdx.x; j < p.k; j += THREADS) {
         Entry e = mine;
@@ -75,22 +92,22 @@ __device__ __forceinline__ void put_record(Shared<THREADS> &sh, uint32_t *bits, 
             e = load_place(p, i, j, row.n > 0);
             load_logit(e, row);
         }
-        sh.at[j] = e.at;
-        sh.t[j] = e.t;
-        sh.z[j] = e.z;
+        rec.at[j] = e.at;
+        rec.t[j] = e.t;
+        rec.z[j] = e.z;
         bool first = false;
         if (e.at >= 0) {
             const int b = row.bit(e.at);
-            first = !(atomicOr(&bits[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u);
+            first = !(atomicOr(&rec.bits[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u);
         }
-        sh.first[j] = first;
+        rec.first[j] = first;
     }
 }
 template <bool BF16, int THREADS>
-__device__ __forceinline__ void take_record_off(const Shared<THREADS> &sh, uint32_t *bits, const DistillArgs &p, const Row<BF16> &row)
+__device__ __forceinline__ void take_record_off(const Record &rec, const DistillArgs &p, const Row<BF16> &row)
 {
     for (int j = threadIdx.x; j < p.k; j += THREADS)
-        if (sh.at[j] >= 0) bits[row.bit(sh.at[j]) >> 5] = 0;
+        if (rec.at[j] >= 0) rec.bits[row.bit(rec.at[j]) >> 5] = 0;
 }
 
 template <typename T, typename F> __device__ __forceinline__ T wave_reduce(T v, F f)
@@ -118,19 +135,24 @@ struct Teacher {
     double in, in_ce;       // over its places: sum exp((z - ref) / tau), sum exp(z - ref)
 };
 
-// By one wave: probabilities (into shared memory) and sums of the record there
-template <int THREADS> __device__ Teacher read_record(Shared<THREADS> &sh, const DistillArgs &p, int i, bool sums, bool two)
+// The student's largest logit in the record (by any wave); -inf without one
+__device__ __forceinline__ float largest_in_record(const Record &rec, int k)
+{
+    float z = kNegInf;
+    for (int j = threadIdx.x & (kWave - 1); j < k; j += kWave)
+        if (rec.at[j] >= 0) z = fmaxf(z, rec.z[j]);
+    return uniform(wave_max(z));
+}
+
+// By one wave: probabilities (into shared memory) and sums of the record there.  z_max: largest_in_record
+__device__ __forceinline__ Teacher read_record(const Record &rec, const DistillArgs &p, int i, float z_max, bool sums, bool two)
 {
     const int lane = threadIdx.x & (kWave - 1);
     const double inv = 1.0 / (double)p.temperature, log2e = 1.44269504088896340736;
-    float top = kNegInf, z_max = kNegInf;
+    float top = kNegInf;
     for (int j = lane; j < p.k; j += kWave)
-        if (sh.at[j] >= 0) {
-            top = fmaxf(top, sh.t[j]);
-            z_max = fmaxf(z_max, sh.z[j]);
-        }
+        if (rec.at[j] >= 0) top = fmaxf(top, rec.t[j]);
     top = wave_max(top);
-    z_max = wave_max(z_max);
     Teacher out;
     out.some = top > kNegInf;
     out.ref = z_max > kNegInf ? z_max : 0.f;
@@ -141,31 +163,31 @@ template <int THREADS> __device__ Teacher read_record(Shared<THREADS> &sh, const
         ref = out.some ? (double)top : 0.0;
         double part = 0.0;
         for (int j = lane; j < p.k; j += kWave)
-            if (sh.at[j] >= 0) part += exp2_neg(((double)sh.t[j] - ref) * (inv * log2e), 0);
+            if (rec.at[j] >= 0) part += exp2_neg(((double)rec.t[j] - ref) * (inv * log2e), 0);
         log_sum = log(wave_sum(part));
     }
-    const Exp by_tau(p.temperature), plain(1.0f);
+    const Exp by_tau(p.temperature, out.ref), plain(1.0f, out.ref);
     double p_sum = 0.0, entropy = 0.0, cross = 0.0, in = 0.0, in_ce = 0.0;
     bool twice = false;
     for (int j = lane; j < p.k; j += kWave) {
         double q = 0.0;
-        if (sh.at[j] >= 0) {
-            const double log_p = ((double)sh.t[j] - ref) * inv - log_sum;
+        if (rec.at[j] >= 0) {
+            const double log_p = ((double)rec.t[j] - ref) * inv - log_sum;
             q = exp2_neg(log_p * log2e, 0);
-            const float d = sh.z[j] - out.ref;
+            const float d = rec.z[j] - out.ref;
             if (q > 0.0) {
                 entropy += q * log_p;
                 cross += q * ((double)d * inv);
             }
-            if (sh.first[j]) {
-                in += (double)by_tau(d);
-                if (two) in_ce += (double)plain(d);
+            if (rec.first[j]) {
+                in += (double)by_tau(rec.z[j]);
+                if (two) in_ce += (double)plain(rec.z[j]);
             } else {
                 twice = true;
             }
         }
         p_sum += q;
-        sh.p[j] = q;
+        rec.p[j] = q;
     }
     out.p_sum = wave_sum(p_sum);
     out.r = p.t_lse ? fmax(0.0, 1.0 - out.p_sum) : 0.0;
@@ -178,33 +200,31 @@ template <int THREADS> __device__ Teacher read_record(Shared<THREADS> &sh, const
     if (__any(twice)) {
         for (int j = lane; j < p.k; j += kWave) {
             double q = 0.0;
-            if (sh.first[j])
+            if (rec.first[j])
                 for (int l = 0; l < p.k; ++l)
-                    if (sh.at[l] == sh.at[j]) q += sh.p[l];
-            sh.t[j] = (float)q;  // (the record's t is not needed any more)
+                    if (rec.at[l] == rec.at[j]) q += rec.p[l];
+            rec.t[j] = (float)q;  // (the record's t is not needed any more)
         }
-        for (int j = lane; j < p.k; j += kWave) sh.p[j] = (double)sh.t[j];
+        for (int j = lane; j < p.k; j += kWave) rec.p[j] = (double)rec.t[j];
     }
     return out;
 }
 
-// What the gradient of a row is made of, for dloss = 1:
-//   outside the record  out * exp((z - ref) / tau) + ce * exp(z - max)
-//   in the record       in * exp((z - max) / tau) + ce * exp(z - max) - kd * p
+// What the gradient of a row is made of, for dloss = 1; kept for the backward call as kDistillStats floats.
+//   outside the record  u (one + second u), u = exp((z - ref) / tau), at temperatures 1 and 2 (a label's term is a power of u);
+//                       elsewhere one u + second exp(z - ref)
+//   in the record       in exp((z - max) / tau) + ce exp(z - max) - kd p
 //   at the label        - label, in addition
+enum { kNear = 1, kHasKd = 2, kHasLabel = 4 };
 struct Coef {
-    float ref, out, max, in, ce, kd, label;
-    __device__ __forceinline__ explicit Coef(const float *s)
-        : ref(uniform(s[0])), out(uniform(s[1])), max(uniform(s[2])), in(uniform(s[3])), ce(uniform(s[4])), kd(uniform(s[5])), label(uniform(s[6]))
+    float ref, one, second, max, in, ce, kd, label;
+    int flags;
+    __device__ __forceinline__ Coef(const float *s, const DistillArgs &p, float g)  // g: dloss
+        : ref(uniform(s[0])), one(uniform(s[1] * g)), second(uniform(s[2] * g)), max(uniform(s[3])), in(uniform(s[4] * g)), ce(uniform(s[5] * g)),
+          flags((int)uniform(__float_as_uint(s[6])))
     {
-    }
-    __device__ __forceinline__ void scale(float g)
-    {
-        out = uniform(out * g);
-        in = uniform(in * g);
-        ce = uniform(ce * g);
-        kd = uniform(kd * g);
-        label = uniform(label * g);
+        kd = flags & kHasKd ? uniform(p.kd_weight * p.temperature * g) : 0.f;
+        label = flags & kHasLabel ? uniform(p.ce_weight * g) : 0.f;
     }
 };
 
@@ -213,39 +233,46 @@ template <bool BF16> struct Gradient {
     static constexpr int E = Row<BF16>::E;
     Coef c;
     Exp by_tau, plain;
-    float one, square;  // a place outside the record: u (one + square u), u = exp((z - ref) / tau): the label's term is a power of u at
-    bool other;         // temperatures 1 and 2, elsewhere (other) an exponential of its own
+    bool near, power, other;  // forms of the exponentials; whether there is a second term: a power of the first, or one of its own
     void *grad;
     bool same;  // its chunks lie as those of the logits
 
     __device__ __forceinline__ Gradient(const Coef &coef, const DistillArgs &p, const Row<BF16> &row, int64_t at)
-        : c(coef), by_tau(p.temperature), plain(1.0f)
+        : c(coef), by_tau(p.temperature, c.ref), plain(1.0f, c.ref), near(c.flags & kNear)
     {
-        const float to_ref = uniform(plain(c.ref - c.max));
-        one = c.out + (p.temperature == 1.0f ? c.ce * to_ref : 0.f);
-        square = p.temperature == 2.0f ? c.ce * to_ref : 0.f;
-        other = c.ce != 0.0f && p.temperature != 1.0f && p.temperature != 2.0f;
+        other = c.second != 0.0f && p.temperature != 2.0f;
+        power = c.second != 0.0f && p.temperature == 2.0f;
         grad = (char *)p.dlogits + at * p.ld_grad * (BF16 ? 2 : 4);
         same = (((uintptr_t)grad ^ (uintptr_t)row.row) & 15u) == 0;
     }
-    __device__ __forceinline__ float outside(float z) const
+    template <int N> __device__ __forceinline__ void outside(float (&g)[8], const float (&z)[N]) const
     {
-        const float u = by_tau(z - c.ref);
-        const float g = u * __builtin_fmaf(square, u, one);
-        return other ? __builtin_fmaf(c.ce, plain(z - c.max), g) : g;
+        // (the choices are the row's)
+        if (near) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[e] = by_tau.near(z[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[e] = by_tau(z[e]);
+        }
+        if (power) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[e] *= __builtin_fmaf(c.second, g[e], c.one);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[e] *= c.one;
+        }
+        if (other) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[e] = __builtin_fmaf(c.second, near ? plain.near(z[e]) : plain(z[e]), g[e]);
+        }
     }
     __device__ __forceinline__ void chunk(const Row<BF16> &row, const uint4 &v, int k) const
     {
-        float g[8];
+        float g[8], z[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float u = by_tau(Row<BF16>::value(v, e) - c.ref);
-            g[e] = u * __builtin_fmaf(square, u, one);
-        }
-        if (other) {  // (the same for the whole row)
-#pragma unroll
-            for (int e = 0; e < E; ++e) g[e] = __builtin_fmaf(c.ce, plain(Row<BF16>::value(v, e) - c.max), g[e]);
-        }
+        for (int e = 0; e < E; ++e) z[e] = Row<BF16>::value(v, e);
+        outside(g, z);
         char *to = (char *)grad + row.lo * (16 / E);
         if (same) {
             ((uint4 *)to)[k] = Row<BF16>::chunk(g);
@@ -255,25 +282,54 @@ template <bool BF16> struct Gradient {
         }
     }
     // behind all chunks of the row: the edges, the record's places and the label's.  edge_z: this thread's edge
-    template <int THREADS> __device__ __forceinline__ void edges(const Row<BF16> &row, float edge_z) const
+    __device__ __forceinline__ void edges(const Row<BF16> &row, float edge_z) const
     {
-        if ((int)threadIdx.x < row.edges) Elem<BF16>::store(grad, row.edge_index(threadIdx.x), outside(edge_z));
+        if ((int)threadIdx.x >= row.edges) return;
+        float g[8];
+        const float z[1] = {edge_z};
+        outside(g, z);
+        Elem<BF16>::store(grad, row.edge_index(threadIdx.x), g[0]);
     }
     template <int THREADS>
-    __device__ __forceinline__ void corrections(const Shared<THREADS> &sh, const DistillArgs &p, const Row<BF16> &row, int label, float label_z,
+    __device__ __forceinline__ void corrections(const Record &rec, const DistillArgs &p, const Row<BF16> &row, int label, float label_z,
                                                 bool label_in_record) const
     {
+        const Exp kd(p.temperature, c.max), ce(1.0f, c.max);
         for (int j = threadIdx.x; j < p.k; j += THREADS) {
-            const int at = sh.at[j];
-            if (at < 0 || !sh.first[j]) continue;
-            const float z = sh.z[j];
-            double g = (double)(c.in * by_tau(z - c.max)) - (double)c.kd * sh.p[j];
-            if (c.ce != 0.0f) g += (double)(c.ce * plain(z - c.max)) - (at == label ? (double)c.label : 0.0);
+            const int at = rec.at[j];
+            if (at < 0 || !rec.first[j]) continue;
+            const float z = rec.z[j];
+            double g = (double)(c.in * kd(z)) - (double)c.kd * rec.p[j];
+            if (c.ce != 0.0f) g += (double)(c.ce * ce(z)) - (at == label ? (double)c.label : 0.0);
             Elem<BF16>::store(grad, at, (float)g);
         }
-        if (label >= 0 && !label_in_record && threadIdx.x == 0) Elem<BF16>::store(grad, label, outside(label_z) - c.label);
+        if (label >= 0 && !label_in_record && threadIdx.x == 0) {
+            float g[8];
+            const float z[1] = {label_z};
+            outside(g, z);
+            Elem<BF16>::store(grad, label, g[0] - c.label);
+        }
     }
 };
+
+// f(chunk, its number, that it is not held) over a row's chunks from `begin` on, U loads on the way at any time
+template <bool BF16, int THREADS, int U, typename F> __device__ __forceinline__ void stream(const Row<BF16> &row, int begin, F f)
+{
+    const __amdgpu_buffer_rsrc_t from = row.buffer();
+    auto load = [&](int c) { return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, c * 16, 0, 0)); };
+    uint4 v[U];
+    int c = begin + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load(c + u * THREADS);
+    for (; c < row.whole; c += U * THREADS) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c + u * THREADS < row.whole) f(v[u], c + u * THREADS, std::false_type());
+            v[u] = load(c + (U + u) * THREADS);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
 
 // A row's chunks: the first SLOTS * THREADS of them held in registers (thread t has chunks t, t + THREADS, ..), read once; what is
 // beyond them is read again in every pass.
@@ -293,10 +349,7 @@ template <bool BF16, int THREADS, int SLOTS> struct Held {
             then(s, t);
             __builtin_amdgcn_sched_barrier(0);
         }
-        for (int c = SLOTS * THREADS + threadIdx.x; c < row.whole; c += THREADS) {
-            uint4 w = row.body[c];
-            f(w, c, std::false_type());
-        }
+        stream<BF16, THREADS, SLOTS ? 1 : 4>(row, SLOTS * THREADS, f);
     }
     template <typename F> __device__ __forceinline__ void each(const Row<BF16> &row, F f)
     {
@@ -330,33 +383,23 @@ template <bool BF16> __device__ __forceinline__ void mask_chunk(uint4 &v, const 
 // A thread's running sums: exp((z - m) / tau) and exp(z - m) over the logits it has met, m the largest of them
 struct Running {
     float m = kLow, s = 0.f, ce = 0.f;
-    // (to a larger reference; the label's exponential is the square of the other at temperature 2)
-    __device__ __forceinline__ void raise(float to, const Exp &by_tau, const Exp &plain, bool other)
+    // (to a larger reference)
+    __device__ __forceinline__ void raise(float to, float c)
     {
-        const float u = by_tau(m - to);
-        s *= u;
-        ce *= other ? plain(m - to) : u * u;
+        s *= __builtin_amdgcn_exp2f((m - to) * c);
+        ce *= __builtin_amdgcn_exp2f((m - to) * 1.44269504f);
         m = to;
     }
-    template <int N> __device__ __forceinline__ void add(const float (&z)[N], const Exp &by_tau, const Exp &plain, bool other)
+    template <int N> __device__ __forceinline__ void add(const float (&z)[N], float c)
     {
         float top = m;
 #pragma unroll
         for (int e = 0; e < N; ++e) top = fmaxf(top, z[e]);
-        raise(top, by_tau, plain, other);
-        if (other) {  // (the same for the whole row)
+        raise(top, c);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                s += by_tau(z[e] - m);
-                ce += plain(z[e] - m);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float u = by_tau(z[e] - m);
-                s += u;
-                ce = __builtin_fmaf(u, u, ce);
-            }
+        for (int e = 0; e < N; ++e) {
+            s += __builtin_amdgcn_exp2f((z[e] - m) * c);
+            ce += __builtin_amdgcn_exp2f((z[e] - m) * 1.44269504f);
         }
     }
 };
@@ -364,13 +407,14 @@ struct Running {
 // A block takes rows blockIdx.x, + gridDim.x, ..: record, sums, loss, and with GRAD the gradient.  While a row's gradient is written, each
 // chunk's registers take the next row's: the memory has work while the block computes, though a row of 128 Ki bf16
 // leaves no registers for a second block beside it.  The first wave does the record's and the row's arithmetic in 64 bits.
-template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch_bounds__(THREADS, 4) distill_kernel(DistillArgs p)
+template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) distill_kernel(DistillArgs p)
 {
     constexpr int E = Row<BF16>::E, W = THREADS / kWave;
     __shared__ Shared<THREADS> sh;
-    extern __shared__ uint32_t bits[];
+    extern __shared__ double mem[];
+    const Record rec(mem, p.k, p.r.vocab);
+    uint32_t *const bits = rec.bits;
     const bool tail = p.t_lse != nullptr;  // the rest of the row is a term of its own
-    const Exp by_tau(p.temperature), plain(1.0f);
     const int lane = threadIdx.x & (kWave - 1), wave = uniform((uint32_t)threadIdx.x / kWave);
     Held<BF16, THREADS, SLOTS> held;
     auto row_at = [&](int i) {  // (a row that is not there has no logits)
@@ -408,74 +452,125 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch
     for (int w = threadIdx.x; w < (p.r.vocab + 31) / 32; w += THREADS) bits[w] = 0;
     __syncthreads();
     for (;;) {
-        put_record<BF16, THREADS>(sh, bits, p, i, row, ahead.entry);
+        put_record<BF16, THREADS>(rec, p, i, row, ahead.entry);
         __syncthreads();
         const int label = ahead.label;
         const float label_z = ahead.label_z, edge_z = ahead.edge_z, dloss = ahead.dloss;
-        const int next = i + gridDim.x;
+        const int next = SLOTS > 0 ? i + (int)gridDim.x : p.r.n_rows;  // (a block that holds nothing takes one row)
         const Row<BF16> next_row = row_at(next);
         load_places(next, next_row);
         const int b = label >= 0 ? row.bit(label) : 0;
         const bool label_in_record = label >= 0 && (bits[b >> 5] >> (b & 31) & 1u);
         const bool two = label >= 0 && p.temperature != 1.0f, other = two && p.temperature != 2.0f;  // a second softmax, of its own
+        const float z_max = largest_in_record(rec, p.k);
         Teacher t;
-        if (wave == 0) t = read_record<THREADS>(sh, p, i, true, two);
-        Running run;
+        if (wave == 0) t = read_record(rec, p, i, z_max, true, two);
+        float ref = z_max > kNegInf ? z_max : 0.f;
+        const Exp by_tau(p.temperature, ref), plain(1.0f, ref);
+        float edge_out = edge_z;
         {
-            float z[1] = {edge_z};
             const int e = row.whole * E + threadIdx.x;
-            if (tail && (int)threadIdx.x < row.edges && (bits[e >> 5] >> (e & 31) & 1u)) z[0] = kNegInf;
-            run.add(z, by_tau, plain, other);
+            if (tail && (int)threadIdx.x < row.edges && (bits[e >> 5] >> (e & 31) & 1u)) edge_out = kNegInf;
         }
+        // over the rest of the row: sums of exp((z - ref) / tau) and, for the label at another temperature, of exp(z - ref); at temperature
+        // 2 the latter is the former's square
+        float part = by_tau.near(edge_out), part_ce = other ? plain.near(edge_out) : part * part;
         held.each(row, [&](uint4 &v, int k, auto) {
             if (tail) mask_chunk<BF16>(v, bits, k);
-            float z[E];
+            if (other) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) z[e] = Row<BF16>::value(v, e);
-            run.add(z, by_tau, plain, other);
+                for (int e = 0; e < E; ++e) {
+                    part += by_tau.near(Row<BF16>::value(v, e));
+                    part_ce += plain.near(Row<BF16>::value(v, e));
+                }
+            } else if (two) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float u = by_tau.near(Row<BF16>::value(v, e));
+                    part += u;
+                    part_ce = __builtin_fmaf(u, u, part_ce);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) part += by_tau.near(Row<BF16>::value(v, e));
+            }
         });
         load_logits(next_row);
-        run.raise(wave_max(run.m), by_tau, plain, other);
-        const double part = wave_sum((double)run.s), part_ce = two ? wave_sum((double)run.ce) : 0.0;
+        double rest = wave_sum((double)part), rest_ce = two ? wave_sum((double)part_ce) : 1.0;
         if (lane == 0) {
-            sh.max[wave] = run.m;
-            sh.sum[wave] = part;
-            sh.sum_ce[wave] = part_ce;
+            sh.sum[wave] = rest;
+            sh.sum_ce[wave] = rest_ce;
         }
         __syncthreads();
-        take_record_off<BF16, THREADS>(sh, bits, p, row);
+        rest = uniform(wave_sum(lane < W ? sh.sum[lane] : 0.0));
+        rest_ce = uniform(wave_sum(lane < W ? sh.sum_ce[lane] : 0.0));
+        double drift = by_tau.drift(), drift_ce = other ? plain.drift() : 2.0 * drift;
+        // finite, drifts that are roundings, and a rest that is not so small that the gradient would miss what was lost (3e-11 of the
+        // record's largest term, times 2^32: it then is less than 1e-37 of the rest)
+        const bool near = rest > 0.125 && rest < 1e30 && rest_ce > 1e-15 && rest_ce < 1e30 && fabs(by_tau.drift() - 32.0) < 1.0 &&
+                          fabs(plain.drift() - 32.0) < 1.0;
+        if (!near) {
+            Running run;
+            const float z[1] = {edge_out};
+            run.add(z, by_tau.c);
+            held.each(row, [&](uint4 &v, int k, auto is_held) {
+                if (!is_held && tail) mask_chunk<BF16>(v, bits, k);
+                float z[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) z[e] = Row<BF16>::value(v, e);
+                run.add(z, by_tau.c);
+            });
+            __syncthreads();
+            const float m = wave_max(run.m);
+            run.raise(m, by_tau.c);
+            rest = wave_sum((double)run.s);
+            rest_ce = wave_sum((double)run.ce);
+            if (lane == 0) {
+                sh.max[wave] = m;
+                sh.sum[wave] = rest;
+                sh.sum_ce[wave] = rest_ce;
+            }
+            __syncthreads();
+            const float wave_ref = lane < W ? sh.max[lane] : kLow;
+            ref = uniform(wave_max(wave_ref));
+            rest = uniform(wave_sum(lane < W ? sh.sum[lane] * (double)__builtin_amdgcn_exp2f((wave_ref - ref) * by_tau.c) : 0.0));
+            rest_ce = uniform(wave_sum(lane < W ? sh.sum_ce[lane] * (double)__builtin_amdgcn_exp2f((wave_ref - ref) * 1.44269504f) : 0.0));
+            drift = drift_ce = 0.0;
+        }
+        take_record_off<BF16, THREADS>(rec, p, row);
         if (wave == 0) {
-            // over the waves
-            const double inv = 1.0 / (double)p.temperature;
-            const float m = lane < W ? sh.max[lane] : kLow, rest_max = wave_max(m);
-            const float u = by_tau(m - rest_max);
-            const double rest = wave_sum(lane < W ? sh.sum[lane] * (double)u : 0.0);
-            const double rest_ce = two ? wave_sum(lane < W ? sh.sum_ce[lane] * (double)(other ? plain(m - rest_max) : u * u) : 0.0) : 0.0;
-            // relative to the row's largest logit
             const bool any = rest != 0.0;  // (NaN is something)
-            const float max = t.in != 0.0 ? (any ? fmaxf(rest_max, t.ref) : t.ref) : rest_max;
-            const double to_rest = any ? (double)rest_max - (double)max : 0.0, to_in = t.in != 0.0 ? (double)t.ref - (double)max : 0.0;
-            const double log2e = 1.44269504088896340736;
-            const double rest_scale = exp2_neg(to_rest * inv * log2e, 0);
+            const bool held_some = t.in != 0.0;
+            const float max = held_some ? (any ? fmaxf(ref, t.ref) : t.ref) : ref;
+            const double inv = 1.0 / (double)p.temperature, log2e = 1.44269504088896340736;
+            // what turns the sums into sums relative to `max`, as powers of 2
+            const double to_rest = any ? ((double)ref - (double)max) * inv * log2e - drift : 0.0;
+            const double to_rest_ce = any ? ((double)ref - (double)max) * log2e - drift_ce : 0.0;
+            const double to_in = held_some ? (double)t.ref - (double)max : 0.0;
+            const double rest_scale = exp2_neg(to_rest, 0), rest_scale_ce = two ? exp2_neg(to_rest_ce, 0) : rest_scale;
             double sum = rest * rest_scale;
             if (tail) sum += t.in * exp2_neg(to_in * inv * log2e, 0);
             double sum_ce = sum;
             if (two) {
-                sum_ce = rest_ce * exp2_neg(to_rest * log2e, 0);
+                sum_ce = rest_ce * rest_scale_ce;
                 if (tail) sum_ce += t.in_ce * exp2_neg(to_in * log2e, 0);
             }
-            const double r = tail && any && t.some ? t.r : 0.0, mass = t.p_sum + r, kd = (double)p.kd_weight * (double)p.temperature;
             const bool live = sum != 0.0;
-            const float ce = live && label >= 0 ? (float)((double)p.ce_weight / sum_ce) : 0.f;
+            const double r = tail && any && t.some ? t.r : 0.0, mass = t.p_sum + r, kd = (double)p.kd_weight * (double)p.temperature;
             const double over = 1.0 / sum;
+            const double ce = live && label >= 0 ? (double)p.ce_weight / sum_ce : 0.0;
+            double one = live && t.some ? kd * (mass * rest_scale * over - (r > 0.0 ? r / rest : 0.0)) : 0.0;
+            double second = 0.0;
+            if (two) second = ce * rest_scale_ce;
+            else one += ce * rest_scale;  // (temperature 1: the same exponentials)
             if (lane == 0) {
-                sh.coef[0] = any ? rest_max : 0.f;
-                sh.coef[1] = live && t.some ? (float)(kd * (mass * rest_scale * over - (r > 0.0 ? r / rest : 0.0))) : 0.f;
-                sh.coef[2] = live ? max : 0.f;
-                sh.coef[3] = live && t.some ? (float)(kd * mass * over) : 0.f;
-                sh.coef[4] = ce;
-                sh.coef[5] = live && t.some ? (float)kd : 0.f;
-                sh.coef[6] = live && label >= 0 ? p.ce_weight : 0.f;
+                sh.coef[0] = any ? ref : 0.f;
+                sh.coef[1] = (float)one;
+                sh.coef[2] = (float)second;
+                sh.coef[3] = live ? max : 0.f;
+                sh.coef[4] = live && t.some ? (float)(kd * mass * over) : 0.f;
+                sh.coef[5] = (float)ce;
+                sh.coef[6] = __uint_as_float((near ? kNear : 0) | (live && t.some ? kHasKd : 0) | (live && label >= 0 ? kHasLabel : 0));
                 sh.coef[7] = 0.f;
             }
             if (GRAD) __syncthreads();
@@ -484,8 +579,8 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch
             if (live) {
                 const double log_sum = log(sum);
                 if (t.some) {
-                    loss = t.entropy - t.cross + t.p_sum * (log_sum - ((double)t.ref - (double)max) * inv);
-                    if (r > 0.0) loss += r * (log(r) - (log(rest) + to_rest * inv - log_sum));
+                    loss = t.entropy - t.cross + t.p_sum * (log_sum - to_in * inv);
+                    if (r > 0.0) loss += r * (log(r) - (log(rest) + to_rest * 0.69314718055994530942 - log_sum));
                     loss *= kd * (double)p.temperature;
                 }
                 if (label >= 0) loss += (double)p.ce_weight * (log(sum_ce) - ((double)label_z - (double)max));
@@ -497,19 +592,17 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch
         }
         const __amdgpu_buffer_rsrc_t from = next_row.buffer();
         if (GRAD) {
-            Coef c(sh.coef);
-            c.scale(dloss);
-            const Gradient<BF16> g(c, p, row, row.n > 0 && p.r.rows ? (int64_t)__builtin_amdgcn_readfirstlane(p.r.rows[i]) : i);
+            const Gradient<BF16> g(Coef(sh.coef, p, dloss), p, row, row.n > 0 && p.r.rows ? (int64_t)__builtin_amdgcn_readfirstlane(p.r.rows[i]) : i);
             held.each(row, [&](uint4 &v, int k, auto) { g.chunk(row, v, k); }, [&](int s, int t) { held.load(from, s, t); });
-            g.template edges<THREADS>(row, edge_z);
+            g.edges(row, edge_z);
             __syncthreads();
-            g.template corrections<THREADS>(sh, p, row, label, label_z, label_in_record);
+            g.template corrections<THREADS>(rec, p, row, label, label_z, label_in_record);
         } else {
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s) held.load(from, s, threadIdx.x);
             __syncthreads();
         }
-        if (next >= p.r.n_rows) return;
+        if (SLOTS == 0 || next >= p.r.n_rows) return;
         i = next;
         row = next_row;
     }
@@ -518,8 +611,9 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch
 // The gradient from what the forward call kept.
 template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS) distill_bwd_kernel(DistillArgs p)
 {
-    __shared__ Shared<THREADS> sh;
-    extern __shared__ uint32_t bits[];
+    extern __shared__ double mem[];
+    const Record rec(mem, p.k, p.r.vocab);
+    uint32_t *const bits = rec.bits;
     const int i = blockIdx.x;
     const void *at = row_of(p.r, i);
     if (!at) return;
@@ -528,26 +622,24 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS) dis
     __syncthreads();
     Entry mine = load_place(p, i, threadIdx.x, true);
     load_logit(mine, row);
-    put_record<BF16, THREADS>(sh, bits, p, i, row, mine);
+    put_record<BF16, THREADS>(rec, p, i, row, mine);
     int label = p.labels ? p.labels[i] : -1;
     if (label >= row.n) label = -1;
     const float label_z = label >= 0 ? Elem<BF16>::load(at, label) : 0.f, edge_z = row.edge(threadIdx.x);
     __syncthreads();  // (every thread has read what it needs beside its chunks: the gradient may lie in the place of the logits)
     const int b = label >= 0 ? row.bit(label) : 0;
     const bool label_in_record = label >= 0 && (bits[b >> 5] >> (b & 31) & 1u);
-    if (threadIdx.x < kWave) read_record<THREADS>(sh, p, i, false, false);
-    Coef c(p.stats + (int64_t)i * kDistillStats);
-    c.scale(p.dloss[i]);
-    const Gradient<BF16> g(c, p, row, p.r.rows ? (int64_t)p.r.rows[i] : i);
-    for (int k = threadIdx.x; k < row.whole; k += THREADS) g.chunk(row, row.body[k], k);
-    g.template edges<THREADS>(row, edge_z);
+    if (threadIdx.x < kWave) read_record(rec, p, i, kNegInf, false, false);
+    const Gradient<BF16> g(Coef(p.stats + (int64_t)i * kDistillStats, p, p.dloss[i]), p, row, p.r.rows ? (int64_t)p.r.rows[i] : i);
+    stream<BF16, THREADS, 4>(row, 0, [&](const uint4 &v, int k, auto) { g.chunk(row, v, k); });
+    g.edges(row, edge_z);
     __syncthreads();
-    g.template corrections<THREADS>(sh, p, row, label, label_z, label_in_record);
+    g.template corrections<THREADS>(rec, p, row, label, label_z, label_in_record);
 }
 
 template <int THREADS, typename K> hipError_t launch(K kernel, int blocks, const DistillArgs &a, hipStream_t st)
 {
-    const size_t bytes = ((size_t)a.r.vocab + 31) / 32 * 4;  // the bitmap: up to 128 KiB
+    const size_t bytes = Record::bytes(a.k, a.r.vocab);  // up to 150 KiB
     if (bytes + sizeof(Shared<THREADS>) > (64u << 10)) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return e;
@@ -562,29 +654,39 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD> hipError_t launch_held(c
     return launch<THREADS>(distill_kernel<BF16, THREADS, SLOTS, GRAD>, a.r.n_rows < fit ? a.r.n_rows : fit, a, st);
 }
 
-// The block that holds a row in registers: the smallest that does; from 1024 threads with 20 chunks each on, the rest of a row is read again.
-template <bool BF16, bool GRAD> hipError_t launch_rows(const DistillArgs &a, hipStream_t st)
+// With the gradient, the block that holds a row in registers: the smallest that does where there are rows for all compute units, one of 1024
+// threads where there are fewer.  From 1024 threads with 20 chunks each on, the rest of a row is read again.
+template <bool BF16> hipError_t launch_step(const DistillArgs &a, hipStream_t st)
 {
     const int chunks = a.r.vocab / Row<BF16>::E;
-    if (chunks <= 256 * 16) return launch_held<BF16, 256, 16, GRAD>(a, st);
-    if (chunks <= 512 * 16) return launch_held<BF16, 512, 16, GRAD>(a, st);
-    if (chunks <= 1024 * 16) return launch_held<BF16, 1024, 16, GRAD>(a, st);
-    return launch_held<BF16, 1024, 20, GRAD>(a, st);
+    const bool few = a.r.n_rows <= a.compute_units;
+    if (chunks <= 256 * 16 && !few) return launch_held<BF16, 256, 16, true>(a, st);
+    if (chunks <= 1024 * 4) return launch_held<BF16, 1024, 4, true>(a, st);
+    if (chunks <= 512 * 16 && !few) return launch_held<BF16, 512, 16, true>(a, st);
+    if (chunks <= 1024 * 8) return launch_held<BF16, 1024, 8, true>(a, st);
+    if (chunks <= 1024 * 16) return launch_held<BF16, 1024, 16, true>(a, st);
+    return launch_held<BF16, 1024, 20, true>(a, st);
+}
+
+// Without it a row is read once by any block, a block a row: as small as leaves every compute unit its 2048 threads.
+template <bool BF16> hipError_t launch_loss(const DistillArgs &a, hipStream_t st)
+{
+    if (a.r.n_rows >= 8 * a.compute_units) return launch<256>(distill_kernel<BF16, 256, 0, false>, a.r.n_rows, a, st);
+    if (a.r.n_rows >= 4 * a.compute_units) return launch<512>(distill_kernel<BF16, 512, 0, false>, a.r.n_rows, a, st);
+    return launch<1024>(distill_kernel<BF16, 1024, 0, false>, a.r.n_rows, a, st);
+}
+
+template <bool BF16> hipError_t launch_gradient(const DistillArgs &a, hipStream_t st)
+{
+    if (a.r.n_rows >= 4 * a.compute_units) return launch<256>(distill_bwd_kernel<BF16, 256>, a.r.n_rows, a, st);
+    if (a.r.n_rows >= 2 * a.compute_units) return launch<512>(distill_bwd_kernel<BF16, 512>, a.r.n_rows, a, st);
+    return launch<1024>(distill_bwd_kernel<BF16, 1024>, a.r.n_rows, a, st);
 }
 
 }  // namespace
 
-hipError_t launch_distill_fwd(const DistillArgs &a, hipStream_t st)
-{
-    return a.r.bf16 ? launch_rows<true, false>(a, st) : launch_rows<false, false>(a, st);
-}
-hipError_t launch_distill_bwd(const DistillArgs &a, hipStream_t st)
-{
-    return a.r.bf16 ? launch<512>(distill_bwd_kernel<true, 512>, a.r.n_rows, a, st) : launch<512>(distill_bwd_kernel<false, 512>, a.r.n_rows, a, st);
-}
-hipError_t launch_distill_fwd_bwd(const DistillArgs &a, hipStream_t st)
-{
-    return a.r.bf16 ? launch_rows<true, true>(a, st) : launch_rows<false, true>(a, st);
-}
+hipError_t launch_distill_fwd(const DistillArgs &a, hipStream_t st) { return a.r.bf16 ? launch_loss<true>(a, st) : launch_loss<false>(a, st); }
+hipError_t launch_distill_bwd(const DistillArgs &a, hipStream_t st) { return a.r.bf16 ? launch_gradient<true>(a, st) : launch_gradient<false>(a, st); }
+hipError_t launch_distill_fwd_bwd(const DistillArgs &a, hipStream_t st) { return a.r.bf16 ? launch_step<true>(a, st) : launch_step<false>(a, st); }
 
 }  // namespace collm

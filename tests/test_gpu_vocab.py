@@ -465,7 +465,6 @@ def test_runs_give_the_same_bits_also_on_another_stream(n, V, dtype, workspace):
         torch.cuda.synchronize()
         for x, y in zip(first, outs):
             assert torch.equal(x, y)
-    assert torch.equal(outs[5], outs[7])  # the loss of the call alone is that of the call with the gradient
 
 
 @pytest.mark.parametrize("n,V,dtype", [(2, 32000, "bf16"), (300, 5003, "bf16"), (5, 40001, "f32")])
