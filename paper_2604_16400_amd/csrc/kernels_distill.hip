@@ -29,6 +29,7 @@ namespace {
 
 using namespace vocab;
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kLow = -3.402823466e+38f;  // the least finite value: a running maximum begins here, so that -inf adds nothing
 
 // exp((z - ref) / tau).  near: 2^32 times that (what is below 2^-126 is lost: this is 2^-158 then), as exp2(z c + b) with b = 32 - ref c
@@ -229,7 +230,7 @@ struct Coef {
 };
 
 // The gradient of one row, place by place
-template <bool BF16> struct Gradient {
+template <bool BF16, bool ONCE> struct Gradient {
     static constexpr int E = Row<BF16>::E;
     Coef c;
     Exp by_tau, plain;
@@ -275,7 +276,8 @@ template <bool BF16> struct Gradient {
         outside(g, z);
         char *to = (char *)grad + row.lo * (16 / E);
         if (same) {
-            ((uint4 *)to)[k] = Row<BF16>::chunk(g);
+            if (ONCE) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, Row<BF16>::chunk(g)), (u32x4 *)to + k);
+            else ((uint4 *)to)[k] = Row<BF16>::chunk(g);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) Elem<BF16>::store(grad, row.lo + (int64_t)k * E + e, g[e]);
@@ -312,28 +314,38 @@ template <bool BF16> struct Gradient {
     }
 };
 
-// f(chunk, its number, that it is not held) over a row's chunks from `begin` on, U loads on the way at any time
-template <bool BF16, int THREADS, int U, typename F> __device__ __forceinline__ void stream(const Row<BF16> &row, int begin, F f)
+// Cache policy of loads and stores that nothing reads again before the last-level cache has lost them: past it.
+constexpr int kOnce = 2;
+template <bool ONCE> __device__ __forceinline__ uint4 load_chunk(__amdgpu_buffer_rsrc_t row, int c)
 {
-    const __amdgpu_buffer_rsrc_t from = row.buffer();
-    auto load = [&](int c) { return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, c * 16, 0, 0)); };
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(row, c * 16, 0, ONCE ? kOnce : 0));
+}
+
+// f(chunk, its number, that it is not held) over a row's chunks from `begin` on, U loads on the way at any time; BACK: the last ones first
+template <bool BF16, int THREADS, int U, bool ONCE, bool BACK, typename F> __device__ __forceinline__ void stream(const Row<BF16> &row, int begin, F f)
+{
+    const __amdgpu_buffer_rsrc_t from = row.buffer();  // (reads outside the row, before it too, give 0)
+    constexpr int kStep = U * THREADS;
+    const int steps = (row.whole - begin + kStep - 1) / kStep;
+    int c = begin + (int)threadIdx.x + (BACK ? (steps - 1) * kStep : 0);
     uint4 v[U];
-    int c = begin + threadIdx.x;
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load(c + u * THREADS);
-    for (; c < row.whole; c += U * THREADS) {
+    for (int u = 0; u < U; ++u) v[u] = load_chunk<ONCE>(from, c + u * THREADS);
+    for (int i = 0; i < steps; ++i) {
+        const int next = BACK ? c - kStep : c + kStep;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (c + u * THREADS < row.whole) f(v[u], c + u * THREADS, std::false_type());
-            v[u] = load(c + (U + u) * THREADS);
+            v[u] = load_chunk<ONCE>(from, next + u * THREADS);
             __builtin_amdgcn_sched_barrier(0);
         }
+        c = next;
     }
 }
 
 // A row's chunks: the first SLOTS * THREADS of them held in registers (thread t has chunks t, t + THREADS, ..), read once; what is
 // beyond them is read again in every pass.
-template <bool BF16, int THREADS, int SLOTS> struct Held {
+template <bool BF16, int THREADS, int SLOTS, bool ONCE> struct Held {
     uint4 v[SLOTS > 0 ? SLOTS : 1];
 
     // f(chunk, its number, whether it is held) over `row`, which is held; the chunk may be changed: what is held keeps the
@@ -349,7 +361,7 @@ template <bool BF16, int THREADS, int SLOTS> struct Held {
             then(s, t);
             __builtin_amdgcn_sched_barrier(0);
         }
-        stream<BF16, THREADS, SLOTS ? 1 : 4>(row, SLOTS * THREADS, f);
+        stream<BF16, THREADS, SLOTS ? 1 : 4, SLOTS == 0 && ONCE, false>(row, SLOTS * THREADS, f);  // (beside what is held it is read again)
     }
     template <typename F> __device__ __forceinline__ void each(const Row<BF16> &row, F f)
     {
@@ -358,7 +370,7 @@ template <bool BF16, int THREADS, int SLOTS> struct Held {
     // (through a buffer descriptor: what is beyond the row's last whole chunk is not read, without a branch)
     __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t row, int s, int t)
     {
-        v[s] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(row, (s * THREADS + t) * 16, 0, 0));
+        v[s] = load_chunk<ONCE>(row, s * THREADS + t);
     }
 };
 
@@ -407,7 +419,7 @@ struct Running {
 // A block takes rows blockIdx.x, + gridDim.x, ..: record, sums, loss, and with GRAD the gradient.  While a row's gradient is written, each
 // chunk's registers take the next row's: the memory has work while the block computes, though a row of 128 Ki bf16
 // leaves no registers for a second block beside it.  The first wave does the record's and the row's arithmetic in 64 bits.
-template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) distill_kernel(DistillArgs p)
+template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) distill_kernel(DistillArgs p)
 {
     constexpr int E = Row<BF16>::E, W = THREADS / kWave;
     __shared__ Shared<THREADS> sh;
@@ -416,7 +428,7 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch
     uint32_t *const bits = rec.bits;
     const bool tail = p.t_lse != nullptr;  // the rest of the row is a term of its own
     const int lane = threadIdx.x & (kWave - 1), wave = uniform((uint32_t)threadIdx.x / kWave);
-    Held<BF16, THREADS, SLOTS> held;
+    Held<BF16, THREADS, SLOTS, ONCE> held;
     auto row_at = [&](int i) {  // (a row that is not there has no logits)
         const void *at = i < p.r.n_rows ? row_of(p.r, i) : nullptr;
         return Row<BF16>(at, at ? p.r.vocab : 0);
@@ -592,7 +604,7 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch
         }
         const __amdgpu_buffer_rsrc_t from = next_row.buffer();
         if (GRAD) {
-            const Gradient<BF16> g(Coef(sh.coef, p, dloss), p, row, row.n > 0 && p.r.rows ? (int64_t)__builtin_amdgcn_readfirstlane(p.r.rows[i]) : i);
+            const Gradient<BF16, ONCE> g(Coef(sh.coef, p, dloss), p, row, row.n > 0 && p.r.rows ? (int64_t)__builtin_amdgcn_readfirstlane(p.r.rows[i]) : i);
             held.each(row, [&](uint4 &v, int k, auto) { g.chunk(row, v, k); }, [&](int s, int t) { held.load(from, s, t); });
             g.edges(row, edge_z);
             __syncthreads();
@@ -608,13 +620,14 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD> __global__ void __launch
     }
 }
 
-// The gradient from what the forward call kept.
-template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS) distill_bwd_kernel(DistillArgs p)
+// The gradient from what the forward call kept.  Rows and their chunks go from the last to the first: the forward call left the last-read
+// ones in the last-level cache.
+template <bool BF16, int THREADS, bool ONCE> __global__ void __launch_bounds__(THREADS, 8) distill_bwd_kernel(DistillArgs p)
 {
     extern __shared__ double mem[];
     const Record rec(mem, p.k, p.r.vocab);
     uint32_t *const bits = rec.bits;
-    const int i = blockIdx.x;
+    const int i = p.r.n_rows - 1 - (int)blockIdx.x;
     const void *at = row_of(p.r, i);
     if (!at) return;
     const Row<BF16> row(at, p.r.vocab);
@@ -630,8 +643,8 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS) dis
     const int b = label >= 0 ? row.bit(label) : 0;
     const bool label_in_record = label >= 0 && (bits[b >> 5] >> (b & 31) & 1u);
     if (threadIdx.x < kWave) read_record(rec, p, i, kNegInf, false, false);
-    const Gradient<BF16> g(Coef(p.stats + (int64_t)i * kDistillStats, p, p.dloss[i]), p, row, p.r.rows ? (int64_t)p.r.rows[i] : i);
-    stream<BF16, THREADS, 4>(row, 0, [&](const uint4 &v, int k, auto) { g.chunk(row, v, k); });
+    const Gradient<BF16, ONCE> g(Coef(p.stats + (int64_t)i * kDistillStats, p, p.dloss[i]), p, row, p.r.rows ? (int64_t)p.r.rows[i] : i);
+    stream<BF16, THREADS, 4, false, true>(row, 0, [&](const uint4 &v, int k, auto) { g.chunk(row, v, k); });
     g.edges(row, edge_z);
     __syncthreads();
     g.template corrections<THREADS>(rec, p, row, label, label_z, label_in_record);
@@ -648,45 +661,64 @@ template <int THREADS, typename K> hipError_t launch(K kernel, int blocks, const
     return hipGetLastError();
 }
 
-template <bool BF16, int THREADS, int SLOTS, bool GRAD> hipError_t launch_held(const DistillArgs &a, hipStream_t st)
+template <bool BF16, int THREADS, int SLOTS, bool ONCE> hipError_t launch_held(const DistillArgs &a, hipStream_t st)
 {
     const int fit = a.compute_units * (1024 / THREADS);  // blocks at a time, by their registers
-    return launch<THREADS>(distill_kernel<BF16, THREADS, SLOTS, GRAD>, a.r.n_rows < fit ? a.r.n_rows : fit, a, st);
+    return launch<THREADS>(distill_kernel<BF16, THREADS, SLOTS, true, ONCE>, a.r.n_rows < fit ? a.r.n_rows : fit, a, st);
 }
+
+// Whether a call's rows are more than the last-level cache (256 MiB) keeps beside their gradient until something reads them again
+bool past_the_cache(const LogitRows &r) { return (int64_t)r.n_rows * r.vocab * (r.bf16 ? 2 : 4) > (int64_t)128 << 20; }
 
 // With the gradient, the block that holds a row in registers: the smallest that does where there are rows for all compute units, one of 1024
 // threads where there are fewer.  From 1024 threads with 20 chunks each on, the rest of a row is read again.
+template <bool BF16, bool ONCE> hipError_t launch_many(const DistillArgs &a, int chunks, hipStream_t st)
+{
+    if (chunks <= 256 * 16) return launch_held<BF16, 256, 16, ONCE>(a, st);
+    if (chunks <= 512 * 16) return launch_held<BF16, 512, 16, ONCE>(a, st);
+    if (chunks <= 1024 * 16) return launch_held<BF16, 1024, 16, ONCE>(a, st);
+    return launch_held<BF16, 1024, 20, ONCE>(a, st);
+}
 template <bool BF16> hipError_t launch_step(const DistillArgs &a, hipStream_t st)
 {
     const int chunks = a.r.vocab / Row<BF16>::E;
-    const bool few = a.r.n_rows <= a.compute_units;
-    if (chunks <= 256 * 16 && !few) return launch_held<BF16, 256, 16, true>(a, st);
-    if (chunks <= 1024 * 4) return launch_held<BF16, 1024, 4, true>(a, st);
-    if (chunks <= 512 * 16 && !few) return launch_held<BF16, 512, 16, true>(a, st);
-    if (chunks <= 1024 * 8) return launch_held<BF16, 1024, 8, true>(a, st);
-    if (chunks <= 1024 * 16) return launch_held<BF16, 1024, 16, true>(a, st);
-    return launch_held<BF16, 1024, 20, true>(a, st);
+    if (past_the_cache(a.r)) return launch_many<BF16, true>(a, chunks, st);
+    if (a.r.n_rows <= a.compute_units) {
+        if (chunks <= 1024 * 4) return launch_held<BF16, 1024, 4, false>(a, st);
+        if (chunks <= 1024 * 8) return launch_held<BF16, 1024, 8, false>(a, st);
+        if (chunks <= 1024 * 16) return launch_held<BF16, 1024, 16, false>(a, st);
+    }
+    return launch_many<BF16, false>(a, chunks, st);
 }
 
 // Without it a row is read once by any block, a block a row: as small as leaves every compute unit its 2048 threads.
-template <bool BF16> hipError_t launch_loss(const DistillArgs &a, hipStream_t st)
+template <bool BF16, bool ONCE> hipError_t launch_loss(const DistillArgs &a, hipStream_t st)
 {
-    if (a.r.n_rows >= 8 * a.compute_units) return launch<256>(distill_kernel<BF16, 256, 0, false>, a.r.n_rows, a, st);
-    if (a.r.n_rows >= 4 * a.compute_units) return launch<512>(distill_kernel<BF16, 512, 0, false>, a.r.n_rows, a, st);
-    return launch<1024>(distill_kernel<BF16, 1024, 0, false>, a.r.n_rows, a, st);
+    if (a.r.n_rows >= 8 * a.compute_units) return launch<256>(distill_kernel<BF16, 256, 0, false, ONCE>, a.r.n_rows, a, st);
+    if (a.r.n_rows >= 4 * a.compute_units) return launch<512>(distill_kernel<BF16, 512, 0, false, ONCE>, a.r.n_rows, a, st);
+    return launch<1024>(distill_kernel<BF16, 1024, 0, false, ONCE>, a.r.n_rows, a, st);
 }
 
-template <bool BF16> hipError_t launch_gradient(const DistillArgs &a, hipStream_t st)
+template <bool BF16, bool ONCE> hipError_t launch_gradient(const DistillArgs &a, hipStream_t st)
 {
-    if (a.r.n_rows >= 4 * a.compute_units) return launch<256>(distill_bwd_kernel<BF16, 256>, a.r.n_rows, a, st);
-    if (a.r.n_rows >= 2 * a.compute_units) return launch<512>(distill_bwd_kernel<BF16, 512>, a.r.n_rows, a, st);
-    return launch<1024>(distill_bwd_kernel<BF16, 1024>, a.r.n_rows, a, st);
+    if (a.r.n_rows >= 4 * a.compute_units) return launch<256>(distill_bwd_kernel<BF16, 256, ONCE>, a.r.n_rows, a, st);
+    if (a.r.n_rows >= 2 * a.compute_units) return launch<512>(distill_bwd_kernel<BF16, 512, ONCE>, a.r.n_rows, a, st);
+    return launch<1024>(distill_bwd_kernel<BF16, 1024, ONCE>, a.r.n_rows, a, st);
 }
 
 }  // namespace
 
-hipError_t launch_distill_fwd(const DistillArgs &a, hipStream_t st) { return a.r.bf16 ? launch_loss<true>(a, st) : launch_loss<false>(a, st); }
-hipError_t launch_distill_bwd(const DistillArgs &a, hipStream_t st) { return a.r.bf16 ? launch_gradient<true>(a, st) : launch_gradient<false>(a, st); }
+hipError_t launch_distill_fwd(const DistillArgs &a, hipStream_t st)
+{
+    // (a backward call, for which `stats` is kept, reads the logits again)
+    if (!a.stats) return a.r.bf16 ? launch_loss<true, true>(a, st) : launch_loss<false, true>(a, st);
+    return a.r.bf16 ? launch_loss<true, false>(a, st) : launch_loss<false, false>(a, st);
+}
+hipError_t launch_distill_bwd(const DistillArgs &a, hipStream_t st)
+{
+    if (past_the_cache(a.r)) return a.r.bf16 ? launch_gradient<true, true>(a, st) : launch_gradient<false, true>(a, st);
+    return a.r.bf16 ? launch_gradient<true, false>(a, st) : launch_gradient<false, false>(a, st);
+}
 hipError_t launch_distill_fwd_bwd(const DistillArgs &a, hipStream_t st) { return a.r.bf16 ? launch_step<true>(a, st) : launch_step<false>(a, st); }
 
 }  // namespace collm
