@@ -143,5 +143,65 @@ __device__ __forceinline__ double exp2_neg(double t, int scale)
     return t < -1000.0 ? 0.0 : __builtin_ldexp(p, (int)n + scale);
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr float kLow = -3.402823466e+38f;  // the least finite value: a running maximum begins here, so that -inf adds nothing
+
+template <typename T, typename F> __device__ __forceinline__ T wave_reduce(T v, F f)
+{
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o));
+    return v;
+}
+template <typename T> __device__ __forceinline__ T wave_sum(T v)
+{
+    return wave_reduce(v, [](T a, T b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+    return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// Cache policy of loads and stores that nothing reads again before the last-level cache has lost them: past it.
+constexpr int kOnce = 2;
+template <bool ONCE> __device__ __forceinline__ uint4 load_chunk(__amdgpu_buffer_rsrc_t row, int c)
+{
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(row, c * 16, 0, ONCE ? kOnce : 0));
+}
+
+// exp((z - ref) / tau).  near: 2^32 times that (what is below 2^-126 is lost: this is 2^-158 then), as exp2(z c + b) with b = 32 - ref c
+// rounded beforehand: the same factor 2^drift in every term, taken out in 64 bits.  Otherwise (ref too large for that) from the difference.
+// The rounding of c and of the argument are errors of |z - ref| / tau 2^-24 each, small where the result is not.
+struct Exp {
+    float c, ref, b;
+    __device__ __forceinline__ Exp(float tau, float r) : c(uniform((float)(1.44269504088896340736 / (double)tau))), ref(r), b(__builtin_fmaf(-r, c, 32.f)) {}
+    __device__ __forceinline__ float near(float z) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, c, b)); }
+    __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z - ref) * c); }
+    __device__ __forceinline__ double drift() const { return (double)ref * (double)c + (double)b; }  // 32, about
+};
+
+// A thread's running sums: exp((z - m) / tau) and exp(z - m) over the logits it has met, m the largest of them
+struct Running {
+    float m = kLow, s = 0.f, ce = 0.f;
+    // (to a larger reference)
+    __device__ __forceinline__ void raise(float to, float c)
+    {
+        s *= __builtin_amdgcn_exp2f((m - to) * c);
+        ce *= __builtin_amdgcn_exp2f((m - to) * 1.44269504f);
+        m = to;
+    }
+    template <int N> __device__ __forceinline__ void add(const float (&z)[N], float c)
+    {
+        float top = m;
+#pragma unroll
+        for (int e = 0; e < N; ++e) top = fmaxf(top, z[e]);
+        raise(top, c);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            s += __builtin_amdgcn_exp2f((z[e] - m) * c);
+            ce += __builtin_amdgcn_exp2f((z[e] - m) * 1.44269504f);
+        }
+    }
+};
+
 }  // namespace vocab
 }  // namespace collm
