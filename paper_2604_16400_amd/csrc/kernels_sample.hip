@@ -8,11 +8,10 @@
 // `want` logits reach, taken from the threads' largest logits so far (the least, over the waves, of the (want / waves)-th largest of
 // a wave's 64).  The list, a few times `want`, is put in order by a counting sort over equal steps of the logit, and all
 // that is asked is read off it in 64 bits.  The sum of the rest need only be near: where its error could change what comes out, and where the
-// list does not reach far enough, the row is done by digits instead (below): exact for every row, in more passes.
+// list does not reach far enough, the row is done by steps instead: exact for every row, in more passes.
 //
-// By digits: the logit's bits, made to rise with the value, are taken 11, 11 and 10 at a time; for each digit a
-// histogram of what is counted (logits, or their weights), over the logits that agree with the digits found so far, and a running sum over its
-// bins say which digit comes next.  Among equal logits the place is a division, and the lowest indices come first.
+// By steps: a histogram of what is counted (logits, or their weights) over equal steps of the logit and a running sum over it say in
+// which step a place lies; the logits of that step are listed, or, if they are too many, taken by smaller steps of their bits.
 //
 // The sums of weights decide by their last bits which token comes out, so they are exact and in no order: each weight is
 // computed in 64 bits and rounded once to a whole multiple of 2^-45 (fewer bits for vocabularies from 2^17 on),
@@ -31,9 +30,13 @@ using namespace vocab;
 
 typedef unsigned long long u64;
 
-constexpr int kBins = 2048;
+constexpr int kBins = 2048;                 // steps of a histogram
 constexpr uint32_t kKeyNone = 0x007fffffu;  // key of -inf: nothing at or below it is ever taken
-constexpr int kTies = 1024;                 // equal logits that are listed at once
+constexpr int kList = 4096;                 // logits listed of a row
+constexpr int kSteps = 1024;                // of the logit, in the counting sort
+constexpr int kQueue = 1536;                // chunks with logits to list
+constexpr int kMost = 256;                  // logits that a row is asked to list
+constexpr int kFew = 512;                   // logits of one step that are listed
 
 // bits that rise with the value; NaN counts as -inf, -0 as 0
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -46,6 +49,12 @@ __device__ __forceinline__ float value_of(uint32_t key)
 {
     return __uint_as_float(key ^ ((key & 0x80000000u) ? 0x80000000u : 0xffffffffu));
 }
+
+// A logit of the row in 64 bits: rising is the order of the row
+__device__ __forceinline__ u64 entry(uint32_t key, int index) { return (u64)~key << 32 | (uint32_t)index; }
+__device__ __forceinline__ uint32_t key_in(u64 entry) { return ~(uint32_t)(entry >> 32); }
+__device__ __forceinline__ float value_in(u64 entry) { return value_of(key_in(entry)); }
+__device__ __forceinline__ int index_in(u64 entry) { return (int)(uint32_t)entry; }
 
 // weights of a row as whole numbers
 struct Weight {
@@ -62,27 +71,25 @@ struct Weight {
     }
 };
 
-constexpr int kList = 4096;   // logits listed of a row
-constexpr int kSteps = 1024;  // of the logit, in the counting sort
-
 template <int THREADS> struct Shared {
+    u64 listed[kList];
     union {
-        struct {  // by digits
-            u64 hist[2][kBins];
-            uint32_t list[kTies];
+        u64 binned[kList];
+        struct {
+            uint4 chunk[kQueue];
+            int chunk_at[kQueue];
         };
-        struct {  // by the list
-            u64 listed[kList], binned[kList];  // ~key above, index below: rising is the order of the row
-            int start[kSteps + 1], fill[kSteps];
-        };
+        u64 hist[2][kBins];
     };
+    int start[kSteps + 1], fill[kSteps];
     u64 wave_sum[THREADS / kWave];
     double red[THREADS / kWave];
     float low[2][THREADS / kWave], top[THREADS / kWave];
-    u64 above;
+    u64 above, found;
+    uint32_t key_min, key_max;
     int bin;
-    uint32_t count;
-    int reach, cut_p[2], cut_m, drawn;
+    int count, queued;
+    int cut_p[2], cut_m, drawn;
     u64 kept;
 };
 
@@ -127,27 +134,26 @@ template <int THREADS> __device__ u64 find_bin(Shared<THREADS> &sh, const u64 *h
     return total;
 }
 
-// A place in the falling order: the q-th lowest index (from 1) among the logits of this key; `above`: what is counted
-// over all greater keys
-struct Place {
-    uint32_t key;
-    uint32_t q;
-    u64 above;
+// What is found by steps: the entry at which a running sum over the order of the row reaches a goal, and the sum before it
+struct Spot {
+    u64 at, above;
 };
 
-template <bool BF16, int THREADS> struct Picker {
+template <bool BF16, int THREADS> struct Steps {
     Shared<THREADS> &sh;
     const Row<BF16> row;
+    float hi, scale;  // the first histogram's steps
 
-    __device__ __forceinline__ Picker(Shared<THREADS> &s, const void *p, int vocab) : sh(s), row(p, vocab) {}
+    __device__ __forceinline__ Steps(Shared<THREADS> &s, const Row<BF16> &r) : sh(s), row(r) {}
 
     // f(key, index) over the row's logits
     template <typename F> __device__ __forceinline__ void each(F f) const
     {
+        constexpr int E = Row<BF16>::E;
         for (int c = threadIdx.x; c < row.whole; c += THREADS) {
             const uint4 v = row.body[c];
 #pragma unroll
-            for (int e = 0; e < Row<BF16>::E; ++e) f(key_of(Row<BF16>::value(v, e)), row.lo + c * Row<BF16>::E + e);
+            for (int e = 0; e < E; ++e) f(key_of(Row<BF16>::value(v, e)), row.lo + c * E + e);
         }
         if ((int)threadIdx.x < row.edges) f(key_of(row.edge(threadIdx.x)), row.edge_index(threadIdx.x));
     }
@@ -156,162 +162,235 @@ template <bool BF16, int THREADS> struct Picker {
         for (int b = threadIdx.x; b < kBins; b += THREADS) hist[b] = 0;
         __syncthreads();
     }
-    static constexpr int kLevels = BF16 ? 2 : 3;  // (a bf16 has no bits below the second digit)
-    static __device__ __forceinline__ int shift(int level) { return level == 0 ? 21 : level == 1 ? 10 : 0; }
-    static __device__ __forceinline__ int bin_of(uint32_t key, int level) { return kBins - 1 - (int)((key >> shift(level)) & (kBins - 1)); }
-
-    // histogram of one digit of the keys that agree with `prefix` above it: what measure(key) gives for each logit, and
-    // `extra` once for the key `extra_key`
-    template <typename M> __device__ __forceinline__ void histogram(u64 *hist, int level, uint32_t prefix, M measure, uint32_t extra_key, u64 extra) const
+    // The first histogram: equal steps from the largest logit down to `lo` and all below it; measure(key, index): what a logit counts
+    // (0: nothing).  Returns the total.
+    template <typename M> __device__ u64 first(float m, float lo, M measure)
     {
-        clear(hist);
-        const uint32_t mask = level == 0 ? 0u : level == 1 ? 0xffe00000u : 0xfffffc00u;
-        auto add = [&](uint32_t key, u64 x) { atomicAdd(&hist[level == 2 ? kBins - 1 - (key & 1023u) : bin_of(key, level)], x); };
-        each([&](uint32_t key, int) {
-            if (key > kKeyNone && (key & mask) == prefix) {
-                const u64 x = measure(key);
-                if (x) add(key, x);
-            }
+        hi = m;
+        scale = fminf((float)(kBins - 1) / (m - lo), 1e30f);
+        if (!(scale >= 0.f)) scale = 0.f;
+        clear(sh.hist[0]);
+        each([&](uint32_t key, int idx) {
+            if (key <= kKeyNone) return;
+            const u64 x = measure(key, idx);
+            if (x) atomicAdd(&sh.hist[0][step(key)], x);
         });
-        if (extra && threadIdx.x == 0 && (extra_key & mask) == prefix) add(extra_key, extra);
         __syncthreads();
+        int bin;
+        u64 above;
+        return find_bin<THREADS>(sh, sh.hist[0], 0, bin, above);
     }
-    // The place at which what is counted reaches `goal`.  first: the histogram of the first digit; measure, extra: as
-    // there; one(key): what one logit of that key counts.
-    template <typename M, typename One>
-    __device__ Place find(const u64 *first, u64 goal, M measure, One one, uint32_t extra_key, u64 extra) const
+    __device__ __forceinline__ int step(uint32_t key) const
+    {
+        return (int)fminf(fmaxf((hi - value_of(key)) * scale, 0.f), (float)(kBins - 1));
+    }
+    // The spot at which what `measure` counts, as in the first histogram, reaches `goal` (1 <= goal <= total)
+    template <typename M> __device__ Spot find(u64 goal, M measure) const
     {
         int bin;
-        u64 above, part;
-        find_bin<THREADS>(sh, first, goal, bin, above);
-        uint32_t prefix = (uint32_t)(kBins - 1 - bin) << 21;
-#pragma unroll
-        for (int level = 1; level < kLevels; ++level) {
-            histogram(sh.hist[1], level, prefix, measure, extra_key, extra);
+        u64 above;
+        find_bin<THREADS>(sh, sh.hist[0], goal, bin, above);
+        uint32_t k_lo = kKeyNone + 1, k_hi = 0xffffffffu;  // the keys in question
+        int shift = -1;                                    // steps of their bits (-1: those of the first histogram)
+        for (;;) {
+            // those of the step
+            if (threadIdx.x == 0) {
+                sh.count = 0;
+                sh.key_min = 0xffffffffu;
+                sh.key_max = 0;
+            }
+            __syncthreads();
+            each([&](uint32_t key, int idx) {
+                if (key < k_lo || key > k_hi || (shift < 0 ? step(key) : (int)((k_hi - key) >> shift)) != bin || !measure(key, idx)) return;
+                const int to = atomicAdd(&sh.count, 1);
+                if (to < kFew) sh.listed[to] = entry(key, idx);
+                atomicMin(&sh.key_min, key);
+                atomicMax(&sh.key_max, key);
+            });
+            __syncthreads();
+            const int count = (int)uniform((uint32_t)sh.count);
+            k_lo = uniform(sh.key_min);
+            k_hi = uniform(sh.key_max);
+            if (count <= kFew) return among(goal, above, count, measure);
+            if (k_lo == k_hi) {
+                // alike: a division says how many, the lowest indices come first
+                const u64 w = measure(k_lo, -1), q = (goal - above + w - 1) / w;
+                return {entry(k_lo, locate(k_lo, (uint32_t)q)), above + (q - 1) * w};
+            }
+            const int bits = 32 - __builtin_clz(k_hi - k_lo);
+            shift = bits > 11 ? bits - 11 : 0;
+            clear(sh.hist[1]);
+            each([&](uint32_t key, int idx) {
+                if (key < k_lo || key > k_hi) return;
+                const u64 x = measure(key, idx);
+                if (x) atomicAdd(&sh.hist[1][(k_hi - key) >> shift], x);
+            });
+            __syncthreads();
+            u64 part;
             find_bin<THREADS>(sh, sh.hist[1], goal - above, bin, part);
             above += part;
-            prefix |= (uint32_t)(kBins - 1 - bin) << (level == 1 ? 10 : 0);
         }
-        if (BF16 && !(prefix & 0x80000000u)) prefix |= 0x3ffu;
-        const u64 w = one(prefix);
-        return {prefix, (uint32_t)((goal - above + w - 1) / w), above};
+    }
+    // the spot among the `count` <= kFew entries listed
+    template <typename M> __device__ Spot among(u64 goal, u64 above, int count, M measure) const
+    {
+        sort_few(count);
+        u64 x = 0, own = 0;
+        if ((int)threadIdx.x < count) {
+            x = sh.listed[kFew + threadIdx.x];
+            own = measure(key_in(x), index_in(x));
+        }
+        u64 incl = own;
+        const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const u64 up = __shfl_up(incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == kWave - 1) sh.wave_sum[wave] = incl;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) incl += sh.wave_sum[w];
+        const u64 before = above + incl - own;
+        if (goal > before && goal <= before + own) {
+            sh.found = x;
+            sh.above = before;
+        }
+        __syncthreads();
+        const Spot out = {uniform(sh.found), uniform(sh.above)};
+        __syncthreads();
+        return out;
+    }
+    // listed[0 .. count) in order to listed[kFew .. ), each behind those before it
+    __device__ __forceinline__ void sort_few(int count) const
+    {
+        for (int t = threadIdx.x; t < count; t += THREADS) {
+            const u64 x = sh.listed[t];
+            int at = 0;
+            for (int j = 0; j < count; ++j) at += sh.listed[j] < x;
+            sh.listed[kFew + at] = x;
+        }
+        __syncthreads();
     }
     // the index of the q-th lowest (from 1) of the logits of one key
     __device__ int locate(uint32_t key, uint32_t q) const
     {
         int lo = 0, width = row.n;  // the indices in question
         for (;;) {
-            if (threadIdx.x == 0) sh.count = 0;
-            __syncthreads();
-            each([&](uint32_t k, int i) {
-                if (k == key && i >= lo && i - lo < width) {
-                    const uint32_t at = atomicAdd(&sh.count, 1u);
-                    if (at < kTies) sh.list[at] = (uint32_t)i;
-                }
-            });
-            __syncthreads();
-            const uint32_t count = sh.count;
-            if (count <= kTies) {
-                for (uint32_t t = threadIdx.x; t < count; t += THREADS) {
-                    const uint32_t mine = sh.list[t];
-                    uint32_t before = 0;
-                    for (uint32_t j = 0; j < count; ++j) before += sh.list[j] < mine;
-                    if (before == q - 1) sh.bin = (int)mine;
-                }
-                __syncthreads();
-                const int found = sh.bin;
-                __syncthreads();
-                return found;
-            }
-            // too many: count them by ranges of indices and go on with the range that holds the q-th
+            // counted by ranges of indices, until a range is one index
             clear(sh.hist[1]);
-            const int step = (width + kBins - 1) / kBins;
+            const int range = (width + kBins - 1) / kBins;
             each([&](uint32_t k, int i) {
-                if (k == key && i >= lo && i - lo < width) atomicAdd(&sh.hist[1][(i - lo) / step], (u64)1);
+                if (k == key && i >= lo && i - lo < width) atomicAdd(&sh.hist[1][(i - lo) / range], (u64)1);
             });
             __syncthreads();
             int bin;
             u64 above;
             find_bin<THREADS>(sh, sh.hist[1], q, bin, above);
             q -= (uint32_t)above;
-            lo += bin * step;
-            width = step;
+            lo += bin * range;
+            width = range;
+            if (range == 1) return lo;
         }
+    }
+    // largest and least logit above -inf (-inf and inf without any)
+    __device__ __forceinline__ void extremes(float &m, float &least) const
+    {
+        m = kNegInf;
+        float neg = kNegInf;
+        each([&](uint32_t key, int) {
+            if (key <= kKeyNone) return;
+            m = fmaxf(m, value_of(key));
+            neg = fmaxf(neg, -value_of(key));
+        });
+        m = block_max<THREADS>(m, sh.red);
+        least = -block_max<THREADS>(neg, sh.red);
     }
 };
 
-// Token and its log probability by digits: every row, whatever its logits.
-template <bool BF16, int THREADS> __device__ void sample_by_digits(Shared<THREADS> &sh, const SampleArgs &p, int i, const void *at, int &token, float &logprob)
+// A row's sampling parameters as they count: k = 0, top_p = 1, min_p = 0 are off
+struct Params {
+    float T, top_p, min_p;
+    int k;
+    bool greedy;
+    __device__ __forceinline__ Params(const SampleArgs &p, int i)
+    {
+        T = uniform(p.temperature ? p.temperature[i] : 1.0f);
+        k = (int)uniform((uint32_t)(p.top_k ? p.top_k[i] : 0));
+        top_p = uniform(p.top_p ? p.top_p[i] : 1.0f);
+        if (!(top_p < 1.0f)) top_p = 1.0f;
+        min_p = uniform(p.min_p ? p.min_p[i] : 0.0f);
+        min_p = min_p > 0.0f ? fminf(min_p, 1.0f) : 0.0f;
+        greedy = !(T > 0.0f) || k == 1;
+        if (k <= 0 || k >= p.r.vocab) k = 0;
+    }
+};
+
+__device__ __forceinline__ Weight weight_of(float m, float T, int vocab)
 {
-    const Picker<BF16, THREADS> pick(sh, at, p.r.vocab);
-    float m = kNegInf;
-    pick.each([&](uint32_t key, int) { m = fmaxf(m, value_of(key)); });
-    m = block_max<THREADS>(m, sh.red);
+    Weight w;
+    w.top_inf = m == __builtin_huge_valf();
+    w.m = m;
+    w.c = 1.44269504088896340736 / (double)T;
+    w.scale = 62 - (32 - __builtin_clz((uint32_t)vocab));
+    if (w.scale > 45) w.scale = 45;
+    return w;
+}
+
+// Token and its log probability by steps: every row, whatever its logits.
+template <bool BF16, int THREADS>
+__device__ void sample_by_steps(Shared<THREADS> &sh, const Row<BF16> &row, const Params &par, float u, int &token, float &logprob)
+{
+    Steps<BF16, THREADS> steps(sh, row);
+    float m, least;
+    steps.extremes(m, least);
     token = -1;
     logprob = kNegInf;
     if (!(m > kNegInf)) return;  // (the same for the whole block, as is every choice below)
-    const float T = p.temperature ? p.temperature[i] : 1.0f;
-    const int k = p.top_k ? p.top_k[i] : 0;
-    const float top_p = p.top_p ? p.top_p[i] : 1.0f;
-    const float min_p = p.min_p && p.min_p[i] > 0.0f ? fminf(p.min_p[i], 1.0f) : 0.0f;
-    if (!(T > 0.0f) || k == 1) {
-        token = pick.locate(key_of(m), 1);
+    auto one = [](uint32_t, int) { return (u64)1; };
+    if (par.greedy) {
+        token = steps.locate(key_of(m), 1);
         logprob = 0.0f;
-    } else {
-        Weight w;
-        w.top_inf = m == __builtin_huge_valf();
-        w.m = m;
-        w.c = 1.44269504088896340736 / (double)T;
-        w.scale = 62 - (32 - __builtin_clz((uint32_t)p.r.vocab));
-        if (w.scale > 45) w.scale = 45;
-        int bin;
-        u64 above;
-        // top-k: of the key at its edge only the lowest indices count, so many of them that there are k logits
-        Place edge = {kKeyNone, 0, 0};
-        if (k > 0 && k < p.r.vocab) {
-            auto one = [](uint32_t) { return (u64)1; };
-            pick.histogram(sh.hist[0], 0, 0, one, 0, 0);
-            if (find_bin<THREADS>(sh, sh.hist[0], 0, bin, above) > (u64)k) edge = pick.find(sh.hist[0], k, one, one, 0, 0);
-        }
-        const u64 extra = edge.q ? w(edge.key) * edge.q : 0;
-        auto inside = [&](uint32_t key) { return key > edge.key ? w(key) : (u64)0; };
-        // min-p: the least key whose weight it keeps, and the sum of the weights it keeps
-        uint32_t key_min = 0;
-        if (min_p > 0.0f && !w.top_inf) {
-            const double low = w.m + (double)T * log((double)min_p);
-            const float f = (float)low;
-            key_min = key_of(f) + ((double)f < low ? 1 : 0);
-        }
-        u64 over = threadIdx.x == 0 && edge.key >= key_min ? extra : 0;
-        pick.histogram(sh.hist[0], 0, 0, [&](uint32_t key) {
-            const u64 x = inside(key);
-            if (key >= key_min) over += x;
-            return x;
-        }, edge.key, extra);
-        u64 kept = find_bin<THREADS>(sh, sh.hist[0], 0, bin, above);
-        if (top_p < 1.0f) {
-            const double goal = ceil((double)top_p * (double)kept);
-            const u64 g = !(goal >= 1.0) ? 1 : goal >= (double)kept ? kept : (u64)goal;
-            const Place last = pick.find(sh.hist[0], g, inside, w, edge.key, extra);
-            kept = last.above + last.q * w(last.key);
-        }
-        if (key_min) {
-            // (both keep a prefix of the order: the shorter one counts)
-            over = block_reduce<u64, THREADS>(over, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
-            kept = over < kept ? over : kept;
-        }
-        const double goal = floor((double)p.u[i] * (double)kept);
-        const u64 g = !(goal >= 0.0) ? 1 : goal >= (double)(kept - 1) ? kept : (u64)goal + 1;
-        const Place drawn = pick.find(sh.hist[0], g, inside, w, edge.key, extra);
-        token = pick.locate(drawn.key, drawn.q);
-        logprob = (float)((w.top_inf ? 0.0 : w.log2_of(drawn.key) * 0.69314718055994530942) - log(__builtin_ldexp((double)kept, -w.scale)));
+        return;
     }
+    const Weight w = weight_of(m, par.T, row.n);
+    u64 last = ~(u64)0;  // the last entry of the top-k
+    if (par.k && steps.first(m, least, one) > (u64)par.k) last = steps.find(par.k, one).at;
+    auto inside = [&](uint32_t key, int idx) { return entry(key, idx < 0 ? 0 : idx) <= last ? w(key) : (u64)0; };
+    // min-p: the least key whose weight it keeps, and the sum of the weights it keeps
+    uint32_t key_min = 0;
+    if (par.min_p > 0.0f && !w.top_inf) {
+        const double low = w.m + (double)par.T * log((double)par.min_p);
+        const float f = (float)low;
+        key_min = key_of(f) + ((double)f < low ? 1 : 0);
+    }
+    u64 over = 0;
+    const u64 total = steps.first(m, fmaxf(least, m - 44.0f * par.T), [&](uint32_t key, int idx) {
+        const u64 x = inside(key, idx);
+        if (key >= key_min) over += x;
+        return x;
+    });
+    u64 kept = total;
+    if (par.top_p < 1.0f) {
+        const double goal = ceil((double)par.top_p * (double)total);
+        const u64 g = !(goal >= 1.0) ? 1 : goal >= (double)total ? total : (u64)goal;
+        const Spot end = steps.find(g, inside);
+        kept = end.above + w(key_in(end.at));
+    }
+    if (key_min) {
+        // (both keep a prefix of the order: the shorter one counts)
+        over = block_reduce<u64, THREADS>(over, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
+        kept = over < kept ? over : kept;
+    }
+    const double goal = floor((double)u * (double)kept);
+    const u64 g = !(goal >= 0.0) ? 1 : goal >= (double)(kept - 1) ? kept : (u64)goal + 1;
+    const u64 drawn = steps.find(g, inside).at;
+    token = index_in(drawn);
+    logprob = (float)((w.top_inf ? 0.0 : w.log2_of(key_in(drawn)) * 0.69314718055994530942) - log(__builtin_ldexp((double)kept, -w.scale)));
 }
 
 // What the one pass found
 struct Found {
     int count;    // listed
-    float bound;  // everything from here on is listed (below it only some of the logits met early)
     bool whole;   // every logit above -inf is listed
     double rest;  // sum of exp((z - ref) / T) over what is not listed
     float ref;
@@ -332,87 +411,100 @@ __device__ __forceinline__ uint32_t rank_in_wave(float v, int rank)
     return at << 16;
 }
 
-// Lists the beginning of the row, at least `want` logits where there are as many, and sums the rest (if `sums`).
+// Lists the beginning of the row, at least `want` logits where there are as many, and sums the rest (if `sums`).  Chunks with a logit to
+// list are put aside, for a thread each to look at later: among the others the pass does not branch.
 template <bool BF16, int THREADS> __device__ Found list_row(Shared<THREADS> &sh, const Row<BF16> &row, int want, bool sums, float tau)
 {
     constexpr int E = Row<BF16>::E, U = 4, W = THREADS / kWave, kRound = U * THREADS;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int rank = (want + W - 1) / W < kWave ? (want + W - 1) / W : kWave;
-    if (threadIdx.x == 0) sh.count = 0;
     const __amdgpu_buffer_rsrc_t from = row.buffer();
     const float edge_z = row.edge(threadIdx.x);
     uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = load_chunk<false>(from, u * THREADS + threadIdx.x);
+    if (threadIdx.x == 0) sh.count = sh.queued = 0;
     float top = fmaxf(edge_z, kNegInf), bound = kLow;
     double rest = 0.0;
     Exp by_T(tau, 0.f);
-    auto take = [&](float z, int idx) {
-        const uint32_t to = atomicAdd(&sh.count, 1u);
-        if (to < kList) sh.listed[to] = ((u64)~key_of(z) << 32) | (uint32_t)idx;
+    auto largest = [&](const uint4 &v) {
+        float m = kNegInf;
+#pragma unroll
+        for (int e = 0; e < E; ++e) m = fmaxf(m, Row<BF16>::value(v, e));
+        return m;
     };
-    for (int r = 0, c = threadIdx.x; r == 0 || r * kRound < row.whole; ++r, c += kRound) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c + u * THREADS < row.whole) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) top = fmaxf(top, Row<BF16>::value(v[u], e));
-            }
+    // the bound from the threads' largest logits so far
+    auto raise_bound = [&](int r) {
         const uint32_t key = rank_in_wave(top, rank);
         if (lane == 0) sh.low[r & 1][wave] = key > kKeyNone ? value_of(key) : kLow;
-        if (r == 0) {
-            const float m = wave_max(top);
-            if (lane == 0) sh.top[wave] = m;
-        }
         __syncthreads();
-        bound = uniform(-wave_max(-sh.low[r & 1][lane & (W - 1)]));
-        bound = fmaxf(bound, kLow);
-        if (r == 0) {
-            const float m = uniform(wave_max(sh.top[lane & (W - 1)]));
-            by_T = Exp(tau, m > kNegInf ? m : 0.f);
-            float z = edge_z;
-            if (z >= bound) {
-                take(z, row.edge_index(threadIdx.x));
-                z = kNegInf;
-            }
-            if (sums) rest += (double)by_T.near(z);
-        }
+        bound = uniform(fmaxf(-wave_max(-sh.low[r & 1][lane & (W - 1)]), kLow));
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (u * THREADS + (int)threadIdx.x < row.whole) top = fmaxf(top, largest(v[u]));
+    {
+        const float m = wave_max(top);
+        if (lane == 0) sh.top[wave] = m;
+    }
+    raise_bound(0);
+    {
+        // (what the sum is relative to: the largest of the first round)
+        const float m = uniform(wave_max(sh.top[lane & (W - 1)]));
+        by_T = Exp(tau, m > kNegInf ? m : 0.f);
+    }
+    int r = 0;
+    for (int c = threadIdx.x; r * kRound < row.whole; ++r, c += kRound) {
+        if (r > 1) raise_bound(r);  // (of the second round nothing is known yet)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (c + u * THREADS < row.whole) {
-                float z[E], m = kNegInf, s = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    z[e] = Row<BF16>::value(v[u], e);
-                    m = fmaxf(m, z[e]);
-                }
+            const int at = c + u * THREADS;
+            if (at < row.whole) {
+                const float m = largest(v[u]);
+                top = fmaxf(top, m);
                 if (m >= bound) {
-                    const int first = row.lo + (c + u * THREADS) * E;
+                    const int to = atomicAdd(&sh.queued, 1);
+                    if (to < kQueue) {
+                        sh.chunk[to] = v[u];
+                        sh.chunk_at[to] = at;
+                    }
+                } else if (sums) {
+                    float s = 0.f;
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (z[e] >= bound) {
-                            take(z[e], first + e);
-                            z[e] = kNegInf;
-                        }
-                }
-                if (sums) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) s += by_T.near(z[e]);
+                    for (int e = 0; e < E; ++e) s += by_T.near(Row<BF16>::value(v[u], e));
                     rest += (double)s;
                 }
             }
-            v[u] = load_chunk<false>(from, c + kRound + u * THREADS);
+            v[u] = load_chunk<false>(from, at + kRound);
         }
+    }
+    if (r > 1) raise_bound(r);
+    else __syncthreads();
+    // everything from the last bound on is listed
+    auto look_at = [&](float z, int idx) {
+        if (z >= bound) {
+            const int to = atomicAdd(&sh.count, 1);
+            if (to < kList) sh.listed[to] = entry(key_of(z), idx);
+        } else if (sums) {
+            rest += (double)by_T.near(z);
+        }
+    };
+    look_at(edge_z, row.edge_index(threadIdx.x));
+    const int queued = (int)uniform((uint32_t)sh.queued);
+    for (int q = threadIdx.x; q < (queued < kQueue ? queued : kQueue); q += THREADS) {
+        const uint4 chunk = sh.chunk[q];
+        const int first = row.lo + sh.chunk_at[q] * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) look_at(Row<BF16>::value(chunk, e), first + e);
     }
     rest = sums ? block_sum<THREADS>(rest, sh.red) : 0.0;
     __syncthreads();
     Found f;
-    f.count = (int)uniform(sh.count);
-    f.bound = bound;
+    f.count = (int)uniform((uint32_t)sh.count);
     f.whole = bound == kLow;
     f.ref = by_T.ref;
     f.rest = rest * exp2_neg(-by_T.drift(), 0);
-    f.ok = f.count <= kList;
+    f.ok = f.count <= kList && queued <= kQueue;
     f.summed = rest < 1e30 && fabs(by_T.drift() - 32.0) < 1.0;
     return f;
 }
@@ -422,7 +514,6 @@ template <int THREADS> __device__ bool sort_list(Shared<THREADS> &sh, int count)
 {
     constexpr int W = THREADS / kWave, N = kList / THREADS, B = kSteps / THREADS;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    auto z_of = [](u64 x) { return value_of(~(uint32_t)(x >> 32)); };
     u64 mine[N];
     float top = kNegInf, low = __builtin_huge_valf();
 #pragma unroll
@@ -430,8 +521,8 @@ template <int THREADS> __device__ bool sort_list(Shared<THREADS> &sh, int count)
         const int e = n * THREADS + threadIdx.x;
         if (e < count) {
             mine[n] = sh.listed[e];
-            top = fmaxf(top, z_of(mine[n]));
-            low = fminf(low, z_of(mine[n]));
+            top = fmaxf(top, value_in(mine[n]));
+            low = fminf(low, value_in(mine[n]));
         }
     }
     top = wave_max(top);
@@ -449,7 +540,7 @@ template <int THREADS> __device__ bool sort_list(Shared<THREADS> &sh, int count)
     if (!(width < __builtin_huge_valf())) return false;
     const float scale = width > 0.f ? (float)(kSteps - 1) / width : 0.f;
     if (!(scale < __builtin_huge_valf())) return false;
-    auto step_of = [&](u64 x) { return (int)fminf((top - z_of(x)) * scale, (float)(kSteps - 1)); };
+    auto step_of = [&](u64 x) { return (int)fminf((top - value_in(x)) * scale, (float)(kSteps - 1)); };
 #pragma unroll
     for (int n = 0; n < N; ++n)
         if (n * THREADS + (int)threadIdx.x < count) atomicAdd(&sh.fill[step_of(mine[n])], 1);
@@ -503,55 +594,34 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     const int i = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const void *at = row_of(p.r, i);
     const Row<BF16> row(at, at ? p.r.vocab : 0);
-    const float T = uniform(p.temperature ? p.temperature[i] : 1.0f);
-    int k = (int)uniform((uint32_t)(p.top_k ? p.top_k[i] : 0));
-    const float top_p = uniform(p.top_p ? p.top_p[i] : 1.0f);
-    float min_p = uniform(p.min_p ? p.min_p[i] : 0.0f);
-    min_p = min_p > 0.0f ? fminf(min_p, 1.0f) : 0.0f;
-    const bool greedy = !(T > 0.0f) || k == 1;
-    if (k <= 0 || k >= p.r.vocab) k = 0;
-    // (of a nucleus or a row that nothing cuts the beginning is 128 logits: where its weights leave too much to the rest, by digits)
-    const int want = greedy ? 1 : k ? (k < kTies ? k : kTies) : 128;
-    const bool sums = !greedy && !k;
-    const Found f = list_row<BF16, THREADS>(sh, row, want, sums, greedy ? 1.0f : T);
+    const Params par(p, i);
+    const float u = uniform(p.u[i]);
+    // (of a nucleus or a row that nothing cuts the beginning is 128 logits)
+    const int want = par.greedy ? 1 : par.k ? par.k : 128;
+    const bool sums = !par.greedy && !par.k;
+    Found f;
+    f.ok = false;
+    if (want <= kMost) f = list_row<BF16, THREADS>(sh, row, want, sums, par.greedy ? 1.0f : par.T);
     int token = -1;
     float logprob = kNegInf;
     bool done = f.ok && f.count == 0;  // nothing above -inf
-    if (!done && f.ok && (!sums || f.summed) && (!k || f.count >= k || f.whole) && sort_list<THREADS>(sh, f.count)) {
-        const float m = value_of(~(uint32_t)(sh.listed[0] >> 32));
-        if (greedy) {
-            token = (int)(uint32_t)sh.listed[0];
+    if (!done && f.ok && (!sums || f.summed) && (!par.k || f.count >= par.k || f.whole) && sort_list<THREADS>(sh, f.count)) {
+        const float m = value_in(sh.listed[0]);
+        if (par.greedy) {
+            token = index_in(sh.listed[0]);
             logprob = 0.0f;
             done = true;
         } else if (m < __builtin_huge_valf()) {
-            Weight w;
-            w.top_inf = false;
-            w.m = m;
-            w.c = 1.44269504088896340736 / (double)T;
-            w.scale = 62 - (32 - __builtin_clz((uint32_t)p.r.vocab));
-            if (w.scale > 45) w.scale = 45;
-            // weights of the list, and their running sum; thread t has entries N t .. N t + N - 1.  The list reaches as far as
-            // the bound: what was listed below it belongs to the rest.
-            if (threadIdx.x == 0) sh.reach = f.count;
-            __syncthreads();
-            u64 own[N], sum = 0, below = 0;
+            const Weight w = weight_of(m, par.T, row.n);
+            // weights of the list, and their running sum; thread t has entries N t .. N t + N - 1
+            const int n_k = par.k && par.k < f.count ? par.k : f.count;
+            u64 own[N], sum = 0;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int e = threadIdx.x * N + n;
-                const uint32_t key = e < f.count ? ~(uint32_t)(sh.listed[e] >> 32) : 0;
-                if (e < f.count && value_of(key) < f.bound) atomicMin(&sh.reach, e);
-            }
-            __syncthreads();
-            const int n_k = k && k < sh.reach ? k : sh.reach;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int e = threadIdx.x * N + n;
-                const u64 x = e < (k ? n_k : f.count) ? w(~(uint32_t)(sh.listed[e] >> 32)) : 0;
-                own[n] = e < n_k ? x : 0;
-                below += e < n_k ? 0 : x;
+                own[n] = e < n_k ? w(key_in(sh.listed[e])) : 0;
                 sum += own[n];
             }
-            if (sums) below = block_reduce<u64, THREADS>(below, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
             u64 incl = sum;
 #pragma unroll
             for (int o = 1; o < kWave; o <<= 1) {
@@ -572,10 +642,10 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
             }
             const u64 first = incl - sum;
             // what the row's weights sum to, at least and at most
-            const double rest = sums ? f.rest * exp2_neg(((double)f.ref - (double)m) * w.c, w.scale) + (double)below : 0.0;
+            const double rest = sums ? f.rest * exp2_neg(((double)f.ref - (double)m) * w.c, w.scale) : 0.0;
             const double all[2] = {(double)listed + rest * (1.0 - 0x1p-17), (double)listed + rest * (1.0 + 0x1p-17)};
-            const double low = (double)m + (double)T * log((double)min_p);
-            if (top_p < 1.0f || min_p > 0.0f) {
+            const double low = (double)m + (double)par.T * log((double)par.min_p);
+            if (par.top_p < 1.0f || par.min_p > 0.0f) {
                 u64 before = first;
 #pragma unroll
                 for (int n = 0; n < N; ++n) {
@@ -583,8 +653,8 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
                     if (e > 0 && e < n_k) {
 #pragma unroll
                         for (int a = 0; a < 2; ++a)
-                            if (top_p < 1.0f && (double)before >= (double)top_p * all[a]) atomicMin(&sh.cut_p[a], e);
-                        if (min_p > 0.0f && (double)value_of(~(uint32_t)(sh.listed[e] >> 32)) < low) atomicMin(&sh.cut_m, e);
+                            if (par.top_p < 1.0f && (double)before >= (double)par.top_p * all[a]) atomicMin(&sh.cut_p[a], e);
+                        if (par.min_p > 0.0f && (double)value_in(sh.listed[e]) < low) atomicMin(&sh.cut_m, e);
                     }
                     before += own[n];
                 }
@@ -592,8 +662,8 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
             }
             const int cut_p = sh.cut_p[0], cut_m = sh.cut_m, n = cut_p < cut_m ? cut_p : cut_m;
             // the list has to reach the cut: as the end of the top-k, of the row, or because something cuts before its end (for certain)
-            const bool ends = n < n_k || k || f.whole;
-            const bool open = !ends && !(top_p < 1.0f) && !(min_p > 0.0f);  // nothing cuts at all
+            const bool ends = n < n_k || par.k || f.whole;
+            const bool open = !ends && !(par.top_p < 1.0f) && !(par.min_p > 0.0f);  // nothing cuts at all
             if ((ends || open) && (sh.cut_p[0] == sh.cut_p[1] || n < cut_p)) {
                 // the weights kept
                 u64 before = first;
@@ -604,13 +674,12 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
                 }
                 __syncthreads();
                 const u64 kept = sh.kept;
-                const double u = (double)p.u[i];
                 // the draw: the first entry whose running sum passes `goal`, for both ends of what the sum may be
                 int drawn[2];
 #pragma unroll
                 for (int a = 0; a < 2; ++a) {
                     const double of = ends ? (double)kept : all[a];
-                    const double goal = u * of;
+                    const double goal = (double)u * of;
                     before = first;
                     if (a == 1) __syncthreads();
                     u64 g = !(goal >= 0.0) ? 0 : (u64)goal;  // (passes: more than that, whole)
@@ -626,9 +695,9 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
                 }
                 if (drawn[0] >= 0 && drawn[0] == drawn[1]) {
                     const u64 x = sh.listed[drawn[0]];
-                    token = (int)(uint32_t)x;
+                    token = index_in(x);
                     const double of = ends ? (double)kept : 0.5 * (all[0] + all[1]);
-                    logprob = (float)(w.log2_of(~(uint32_t)(x >> 32)) * 0.69314718055994530942 - log(__builtin_ldexp(of, -w.scale)));
+                    logprob = (float)(w.log2_of(key_in(x)) * 0.69314718055994530942 - log(__builtin_ldexp(of, -w.scale)));
                     done = true;
                 }
             }
@@ -636,7 +705,7 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     }
     if (!done) {
         __syncthreads();
-        sample_by_digits<BF16, THREADS>(sh, p, i, at, token, logprob);
+        sample_by_steps<BF16, THREADS>(sh, row, par, u, token, logprob);
     }
     if (threadIdx.x == 0) {
         p.token[i] = token;
@@ -644,20 +713,22 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     }
 }
 
-// One block a row, as above; a list that is too long: by digits, the k-th place by counting, then the k logits up to it.
+// One block a row, as above; a list that is too long: by steps, the k-th place by counting, then the k logits up to it.
 template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) top_kernel(TopArgs p)
 {
     __shared__ Shared<THREADS> sh;
     const int i = blockIdx.x;
     const void *at = row_of(p.r, i);
     const Row<BF16> row(at, at ? p.r.vocab : 0);
-    Found f = list_row<BF16, THREADS>(sh, row, p.k, p.lse != nullptr, p.temperature);
+    Found f;
+    f.ok = f.summed = false;
+    if (p.k <= kMost) f = list_row<BF16, THREADS>(sh, row, p.k, p.lse != nullptr, p.temperature);
     double sum = 0.0;  // of exp((z - ref) / temperature)
     bool sorted = f.ok && (f.count >= p.k || f.whole) && sort_list<THREADS>(sh, f.count);
-    if (p.lse && f.ok && f.summed) {
+    if (p.lse && sorted && f.summed) {
         const double c = 1.44269504088896340736 / (double)p.temperature;
-        for (int e = threadIdx.x; sorted && e < f.count; e += THREADS)
-            sum += exp2_neg(((double)value_of(~(uint32_t)(sh.listed[e] >> 32)) - (double)f.ref) * c, 0);
+        for (int e = threadIdx.x; e < f.count; e += THREADS)
+            sum += exp2_neg(((double)value_in(sh.listed[e]) - (double)f.ref) * c, 0);
     }
     if (p.lse && !(sorted && f.summed)) {
         // (relative to each thread's largest logit; of the logits as they are: a NaN among them shows)
@@ -682,29 +753,23 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     }
     if (!sorted) {
         __syncthreads();
-        const Picker<BF16, THREADS> pick(sh, at, row.n);
-        auto one = [](uint32_t) { return (u64)1; };
-        pick.histogram(sh.hist[0], 0, 0, one, 0, 0);
-        int bin;
-        u64 above;
-        const u64 finite = find_bin<THREADS>(sh, sh.hist[0], 0, bin, above);
-        uint32_t edge = kKeyNone + 1;  // the least key taken, and its last index
-        int last = p.r.vocab;
-        if (finite > (u64)p.k) {
-            const Place place = pick.find(sh.hist[0], p.k, one, one, 0, 0);
-            edge = place.key;
-            last = pick.locate(place.key, place.q);
-        }
+        Steps<BF16, THREADS> steps(sh, row);
+        float m, least;
+        steps.extremes(m, least);
+        auto one = [](uint32_t, int) { return (u64)1; };
+        u64 last = ~(u64)0;
+        if (steps.first(m, least, one) > (u64)p.k) last = steps.find(p.k, one).at;
         if (threadIdx.x == 0) sh.count = 0;
         __syncthreads();
-        pick.each([&](uint32_t key, int idx) {
-            if (key > edge || (key == edge && idx <= last)) {
-                const uint32_t to = atomicAdd(&sh.count, 1u);
-                if (to < kMaxTop) sh.binned[to] = ((u64)~key << 32) | (uint32_t)idx;
+        steps.each([&](uint32_t key, int idx) {
+            const u64 x = entry(key, idx);
+            if (key > kKeyNone && x <= last) {
+                const int to = atomicAdd(&sh.count, 1);
+                if (to < kMaxTop) sh.binned[to] = x;
             }
         });
         __syncthreads();
-        f.count = (int)sh.count;  // min(k, finite)
+        f.count = (int)uniform((uint32_t)sh.count);  // min(k, logits above -inf)
         for (int t = threadIdx.x; t < f.count; t += THREADS) {
             const u64 x = sh.binned[t];
             int before = 0;
@@ -718,8 +783,8 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     for (int t = threadIdx.x; t < p.k; t += THREADS) {
         const bool there = t < f.count;
         const u64 x = there ? sh.listed[t] : 0;
-        values[t] = there ? value_of(~(uint32_t)(x >> 32)) : kNegInf;
-        indices[t] = there ? (int32_t)(uint32_t)x : -1;
+        values[t] = there ? value_in(x) : kNegInf;
+        indices[t] = there ? index_in(x) : -1;
     }
 }
 
