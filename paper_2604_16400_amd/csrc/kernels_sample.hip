@@ -10,6 +10,10 @@
 // that is asked is read off it in 64 bits.  The sum of the rest need only be near: where its error could change what comes out, and where the
 // list does not reach far enough, the row is done by steps instead: exact for every row, in more passes.
 //
+// Rows of bf16 that are cut by their weights are not listed: they have few different logits.  One pass counts each (the 2047 of least
+// magnitude apart that 16 octaves of either sign hold; what lies nearer to 0 is listed), a weight is computed once for each
+// that occurs, and a running sum over them gives every place.  Only the token's index needs the row again.
+//
 // By steps: a histogram of what is counted (logits, or their weights) over equal steps of the logit and a running sum over it say in
 // which step a place lies; the logits of that step are listed, or, if they are too many, taken by smaller steps of their bits.
 //
@@ -31,6 +35,7 @@ using namespace vocab;
 typedef unsigned long long u64;
 
 constexpr int kBins = 2048;                 // steps of a histogram
+constexpr int kSlots = 4096;                // logits that are counted by value
 constexpr uint32_t kKeyNone = 0x007fffffu;  // key of -inf: nothing at or below it is ever taken
 constexpr int kList = 4096;                 // logits listed of a row
 constexpr int kSteps = 1024;                // of the logit, in the counting sort
@@ -80,6 +85,7 @@ template <int THREADS> struct Shared {
             int chunk_at[kQueue];
         };
         u64 hist[2][kBins];
+        uint32_t times[kSlots];
     };
     int start[kSteps + 1], fill[kSteps];
     u64 wave_sum[THREADS / kWave];
@@ -146,14 +152,24 @@ template <bool BF16, int THREADS> struct Steps {
 
     __device__ __forceinline__ Steps(Shared<THREADS> &s, const Row<BF16> &r) : sh(s), row(r) {}
 
-    // f(key, index) over the row's logits
+    // f(key, index) over the row's logits, four loads on the way at any time
     template <typename F> __device__ __forceinline__ void each(F f) const
     {
-        constexpr int E = Row<BF16>::E;
-        for (int c = threadIdx.x; c < row.whole; c += THREADS) {
-            const uint4 v = row.body[c];
+        constexpr int E = Row<BF16>::E, U = 4;
+        const __amdgpu_buffer_rsrc_t from = row.buffer();
+        uint4 v[U];
 #pragma unroll
-            for (int e = 0; e < E; ++e) f(key_of(Row<BF16>::value(v, e)), row.lo + c * E + e);
+        for (int u = 0; u < U; ++u) v[u] = load_chunk<false>(from, u * THREADS + threadIdx.x);
+        for (int c = threadIdx.x; c < row.whole; c += U * THREADS) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = c + u * THREADS;
+                if (at < row.whole) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) f(key_of(Row<BF16>::value(v[u], e)), row.lo + at * E + e);
+                }
+                v[u] = load_chunk<false>(from, at + U * THREADS);
+            }
         }
         if ((int)threadIdx.x < row.edges) f(key_of(row.edge(threadIdx.x)), row.edge_index(threadIdx.x));
     }
@@ -388,6 +404,278 @@ __device__ void sample_by_steps(Shared<THREADS> &sh, const Row<BF16> &row, const
     logprob = (float)((w.top_inf ? 0.0 : w.log2_of(key_in(drawn)) * 0.69314718055994530942) - log(__builtin_ldexp((double)kept, -w.scale)));
 }
 
+// The index of the q-th lowest (from 1) of the logits whose bf16 bits are `bits` (not a zero's): counted by runs of 128 chunks,
+// then within the run.
+template <int THREADS> __device__ int locate_bits(Shared<THREADS> &sh, const Row<true> &row, uint32_t bits, uint32_t q)
+{
+    constexpr int U = 4, kRun = 2 * kWave;
+    const int lane = threadIdx.x & (kWave - 1), runs = (row.whole + kRun - 1) / kRun;
+    auto in_chunk = [&](const uint4 &v) {  // one bit an element
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m |= ((w[j] & 0xffffu) == bits ? 1u << (2 * j) : 0u) | ((w[j] >> 16) == bits ? 2u << (2 * j) : 0u);
+        return m;
+    };
+    // bins: the edges in front, the runs, the edges behind
+    u64 *const hist = sh.hist[0];
+    for (int r = threadIdx.x; r < kBins; r += THREADS) hist[r] = 0;
+    __syncthreads();
+    const bool at_edge = (int)threadIdx.x < row.edges && ((const uint16_t *)row.row)[row.edge_index(threadIdx.x)] == (uint16_t)bits;
+    if (at_edge) atomicAdd(&hist[(int)threadIdx.x < row.lo ? 0 : 1 + runs], (u64)1);
+    const __amdgpu_buffer_rsrc_t from = row.buffer();
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_chunk<false>(from, u * THREADS + threadIdx.x);
+    for (int c = threadIdx.x; c < row.whole; c += U * THREADS) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = c + u * THREADS;
+            if (at < row.whole) {
+                const uint32_t m = in_chunk(v[u]);
+                if (m) atomicAdd(&hist[1 + at / kRun], (u64)__popc(m));
+            }
+            v[u] = load_chunk<false>(from, at + U * THREADS);
+        }
+    }
+    __syncthreads();
+    int bin;
+    u64 above;
+    find_bin<THREADS>(sh, hist, q, bin, above);
+    const int nth = (int)(q - (uint32_t)above);  // in the bin, from 1
+    if (threadIdx.x < kWave) {
+        // (edges are the first wave's; of a run a lane has two chunks)
+        const bool mine = at_edge && ((int)threadIdx.x < row.lo ? 0 : 1 + runs) == bin;
+        const int c = (bin - 1) * kRun + 2 * lane;
+        uint32_t m = mine ? 1 : 0;
+        if (bin > 0 && bin <= runs) {
+            m = c < row.whole ? in_chunk(row.body[c]) : 0;
+            if (c + 1 < row.whole) m |= in_chunk(row.body[c + 1]) << 8;
+        }
+        int incl = __popc(m);
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int up = __shfl_up(incl, o);
+            if (lane >= o) incl += up;
+        }
+        const int before = incl - __popc(m);
+        if (nth > before && nth <= incl) {
+            for (int k = before + 1; k < nth; ++k) m &= m - 1;
+            sh.bin = bin > 0 && bin <= runs ? row.lo + c * 8 + __ffs(m) - 1 : row.edge_index(threadIdx.x);
+        }
+    }
+    __syncthreads();
+    const int found = (int)uniform((uint32_t)sh.bin);
+    __syncthreads();
+    return found;
+}
+
+// Token and log probability of a row of bf16 by counting how often each logit occurs; false: not that kind of row (a largest logit far beyond
+// those of the row's first round, NaN among the logits, many near 0).
+//   slots 0 .. 2047: positive logits, falling; 2048: those nearer to 0 than any slot, listed; 2049 ..: negative ones
+template <int THREADS>
+__device__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const Params &par, float u, int &token, float &logprob)
+{
+    constexpr int U = 4, N = kSlots / THREADS, W = THREADS / kWave, kZero = 2048;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const __amdgpu_buffer_rsrc_t from = row.buffer();
+    uint4 v[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) v[k] = load_chunk<false>(from, k * THREADS + threadIdx.x);
+    const float edge_z = row.edge(threadIdx.x);
+    for (int k = threadIdx.x; k < kSlots; k += THREADS) sh.times[k] = 0;
+    if (threadIdx.x == 0) {
+        sh.count = 0;
+        sh.queued = 0;
+    }
+    float top = fmaxf(edge_z, kNegInf);
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+        if (k * THREADS + (int)threadIdx.x < row.whole) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, Row<true>::value(v[k], e));
+        }
+    top = block_max<THREADS>(top, sh.red);
+    if (!(top > kNegInf)) return false;
+    // 16 octaves: the uppermost above that of the first round's largest logit and of what weighs nothing beside it
+    const float reach = fmaxf(fabsf(top), fminf(fabsf(top - 44.0f * par.T), 3e38f));
+    const int last = (int)((__float_as_uint(reach) >> 16) | 0x7fu) + 0x80;  // greatest magnitude with a slot, in bf16 bits
+    const int base = last - 2047;                                          // least
+    if (last >= 0x7f80 || base <= 0) return false;
+    auto count = [&](uint32_t h, int idx) {
+        const int mag = (int)(h & 0x7fffu) - base;
+        if ((uint32_t)mag < 2047u + (h < 0x8000u ? 1u : 0u)) {
+            atomicAdd(&sh.times[h < 0x8000u ? 2047 - mag : 2049 + mag], 1u);
+        } else if (mag < 0) {
+            const int to = atomicAdd(&sh.count, 1);
+            if (to < kFew) sh.listed[to] = entry(key_of(bf16_to_f32(h)), idx);
+        } else if (h < 0x8000u || h > 0xff80u) {
+            sh.queued = 1;  // beyond the slots, or NaN
+        }
+    };
+    if ((int)threadIdx.x < row.edges) count(((const uint16_t *)row.row)[row.edge_index(threadIdx.x)], row.edge_index(threadIdx.x));
+    for (int c = threadIdx.x; c < row.whole; c += U * THREADS) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int at = c + k * THREADS;
+            if (at < row.whole) {
+                const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) count((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu, row.lo + at * 8 + e);
+            }
+            v[k] = load_chunk<false>(from, at + U * THREADS);
+        }
+    }
+    __syncthreads();
+    const int near_zero = (int)uniform((uint32_t)sh.count);
+    if (uniform((uint32_t)sh.queued) || near_zero > kFew) return false;
+    if (near_zero) Steps<true, THREADS>(sh, row).sort_few(near_zero);
+    // thread t has slots N t .. N t + N - 1
+    uint32_t times[N];
+    int first = kSlots;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int slot = threadIdx.x * N + n;
+        times[n] = slot == kZero ? (uint32_t)near_zero : sh.times[slot];
+        if (times[n] && first == kSlots) first = slot;
+    }
+    first = (int)-block_max<THREADS>((float)-first, sh.red);  // of the largest logit
+    auto key_at = [&](int slot) {  // (not of kZero)
+        const uint32_t h = slot < kZero ? (uint32_t)(base + 2047 - slot) : 0x8000u | (uint32_t)(base + slot - 2049);
+        return key_of(bf16_to_f32(h));
+    };
+    const u64 *zeros = sh.listed + kFew;
+    if (first == kSlots) return false;
+    const float m = first == kZero ? value_in(zeros[0]) : value_of(key_at(first));
+    const Weight w = weight_of(m, par.T, row.n);
+    // how many the top-k keeps of each slot
+    if (par.k) {
+        int incl = 0, own = 0;
+#pragma unroll
+        for (int n = 0; n < N; ++n) own += (int)times[n];
+        incl = own;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int up = __shfl_up(incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == kWave - 1) sh.wave_sum[wave] = (u64)incl;
+        __syncthreads();
+        int run = incl - own, all = 0;
+        for (int k = 0; k < W; ++k) {
+            if (k < wave) run += (int)sh.wave_sum[k];
+            all += (int)sh.wave_sum[k];
+        }
+        __syncthreads();
+        if (all < par.k) return false;  // (some may lie below the slots)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int left = par.k - run;
+            run += (int)times[n];
+            times[n] = left <= 0 ? 0 : (uint32_t)left < times[n] ? (uint32_t)left : times[n];
+        }
+    }
+    // weights, and those that min-p keeps
+    double low = kNegInf;
+    if (par.min_p > 0.0f) low = w.m + (double)par.T * log((double)par.min_p);
+    u64 one[N], own[N], sum = 0, over = 0, of_zeros = 0;
+    u64 *const weight_of_zero = sh.listed + 2 * kFew;
+    if (near_zero) {
+        if (threadIdx.x == kZero / N) sh.cut_m = (int)times[kZero % N];
+        __syncthreads();
+        u64 x = 0;
+        if ((int)threadIdx.x < sh.cut_m) {
+            x = w(key_in(zeros[threadIdx.x]));
+            if ((double)value_in(zeros[threadIdx.x]) >= low) over = x;
+            weight_of_zero[threadIdx.x] = x;
+        }
+        of_zeros = block_reduce<u64, THREADS>(x, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int slot = threadIdx.x * N + n;
+        one[n] = own[n] = 0;
+        if (!times[n]) continue;
+        if (slot == kZero) {
+            own[n] = of_zeros;
+        } else {
+            one[n] = w(key_at(slot));
+            own[n] = one[n] * times[n];
+            if ((double)value_of(key_at(slot)) >= low) over += own[n];
+        }
+        sum += own[n];
+    }
+    u64 incl = sum;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const u64 up = __shfl_up(incl, o);
+        if (lane >= o) incl += up;
+    }
+    if (lane == kWave - 1) sh.wave_sum[wave] = incl;
+    __syncthreads();
+    u64 total = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        if (k == wave) incl += total;
+        total += sh.wave_sum[k];
+    }
+    __syncthreads();
+    const u64 begin = incl - sum;
+    // where the running sum reaches `goal`: the slot, how many of it (from 1), and the sum with those
+    auto find = [&](u64 goal, int &slot, uint32_t &q, u64 &with) {
+        if (goal > begin && goal <= incl) {
+            u64 run = begin;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (goal > run && goal <= run + own[n]) {
+                    const int at = threadIdx.x * N + n;
+                    uint32_t many = 0;
+                    u64 x = run;
+                    if (at == kZero) {
+                        while (x < goal) x += weight_of_zero[many++];
+                    } else {
+                        many = (uint32_t)((goal - run + one[n] - 1) / one[n]);
+                        x += many * one[n];
+                    }
+                    sh.bin = at;
+                    sh.drawn = (int)many;
+                    sh.above = x;
+                }
+                run += own[n];
+            }
+        }
+        __syncthreads();
+        slot = (int)uniform((uint32_t)sh.bin);
+        q = uniform((uint32_t)sh.drawn);
+        with = uniform(sh.above);
+        __syncthreads();
+    };
+    int slot;
+    uint32_t q;
+    u64 kept = total, with;
+    if (par.top_p < 1.0f) {
+        const double goal = ceil((double)par.top_p * (double)total);
+        find(!(goal >= 1.0) ? 1 : goal >= (double)total ? total : (u64)goal, slot, q, kept);
+    }
+    if (par.min_p > 0.0f) {
+        // (both keep a prefix of the order: the shorter one counts)
+        over = block_reduce<u64, THREADS>(over, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
+        kept = over < kept ? over : kept;
+    }
+    const double goal = floor((double)u * (double)kept);
+    find(!(goal >= 0.0) ? 1 : goal >= (double)(kept - 1) ? kept : (u64)goal + 1, slot, q, with);
+    uint32_t key;
+    if (slot == kZero) {
+        key = key_in(zeros[q - 1]);
+        token = index_in(zeros[q - 1]);
+    } else {
+        key = key_at(slot);
+        token = locate_bits<THREADS>(sh, row, __float_as_uint(value_of(key)) >> 16, q);
+    }
+    logprob = (float)(w.log2_of(key) * 0.69314718055994530942 - log(__builtin_ldexp((double)kept, -w.scale)));
+    return true;
+}
+
 // What the one pass found
 struct Found {
     int count;    // listed
@@ -599,12 +887,18 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     // (of a nucleus or a row that nothing cuts the beginning is 128 logits)
     const int want = par.greedy ? 1 : par.k ? par.k : 128;
     const bool sums = !par.greedy && !par.k;
-    Found f;
-    f.ok = false;
-    if (want <= kMost) f = list_row<BF16, THREADS>(sh, row, want, sums, par.greedy ? 1.0f : par.T);
     int token = -1;
     float logprob = kNegInf;
-    bool done = f.ok && f.count == 0;  // nothing above -inf
+    bool done = false;
+    if constexpr (BF16)
+        if (!par.greedy && (!par.k || par.k > kMost)) done = sample_by_slots<THREADS>(sh, row, par, u, token, logprob);
+    Found f;
+    f.ok = false;
+    if (!done && want <= kMost) {
+        if (BF16 && sums) __syncthreads();
+        f = list_row<BF16, THREADS>(sh, row, want, sums, par.greedy ? 1.0f : par.T);
+        done = f.ok && f.count == 0;  // nothing above -inf
+    }
     if (!done && f.ok && (!sums || f.summed) && (!par.k || f.count >= par.k || f.whole) && sort_list<THREADS>(sh, f.count)) {
         const float m = value_in(sh.listed[0]);
         if (par.greedy) {
