@@ -25,8 +25,8 @@ FLAGS = [
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 
-# kernels that hold a row in registers through a loop over rows: constants of the loop moved in front of it would take the row's registers
-SOURCE_FLAGS = {"kernels_distill.hip": ["-mllvm", "-disable-machine-licm"]}
+# kernels whose loops over a row leave few registers: constants of their 64-bit arithmetic moved in front of the loops would take those
+SOURCE_FLAGS = {name: ["-mllvm", "-disable-machine-licm"] for name in ("kernels_distill.hip", "kernels_sample.hip")}
 
 
 def _stale(out: str, deps) -> bool:

@@ -10,9 +10,9 @@
 // that is asked is read off it in 64 bits.  The sum of the rest need only be near: where its error could change what comes out, and where the
 // list does not reach far enough, the row is done by steps instead: exact for every row, in more passes.
 //
-// Rows of bf16 that are cut by their weights are not listed: they have few different logits.  One pass counts each (the 2047 of least
-// magnitude apart that 16 octaves of either sign hold; what lies nearer to 0 is listed), a weight is computed once for each
-// that occurs, and a running sum over them gives every place.  Only the token's index needs the row again.
+// Rows of bf16 that are cut by their weights are not listed: they have few different logits.  One pass counts each (of either sign those of
+// 32 octaves, 2^-15 to 2^17; what lies nearer to 0 is listed), a weight is computed once for each that occurs, and a running sum
+// over them gives every place.  Only the token's index needs the row again.
 //
 // By steps: a histogram of what is counted (logits, or their weights) over equal steps of the logit and a running sum over it say in
 // which step a place lies; the logits of that step are listed, or, if they are too many, taken by smaller steps of their bits.
@@ -35,7 +35,7 @@ using namespace vocab;
 typedef unsigned long long u64;
 
 constexpr int kBins = 2048;                 // steps of a histogram
-constexpr int kSlots = 4096;                // logits that are counted by value
+constexpr int kSlots = 8192;                // logits that are counted by value
 constexpr uint32_t kKeyNone = 0x007fffffu;  // key of -inf: nothing at or below it is ever taken
 constexpr int kList = 4096;                 // logits listed of a row
 constexpr int kSteps = 1024;                // of the logit, in the counting sort
@@ -90,7 +90,7 @@ template <int THREADS> struct Shared {
     int start[kSteps + 1], fill[kSteps];
     u64 wave_sum[THREADS / kWave];
     double red[THREADS / kWave];
-    float low[2][THREADS / kWave], top[THREADS / kWave];
+    float low[2][THREADS / kWave], top[THREADS / kWave], all[THREADS / kWave];
     u64 above, found;
     uint32_t key_min, key_max;
     int bin;
@@ -101,7 +101,7 @@ template <int THREADS> struct Shared {
 
 // The first bin at which the running sum over the bins reaches `goal` (1 <= goal <= total), and the sum before it;
 // returns the total.  goal 0: the total alone.
-template <int THREADS> __device__ u64 find_bin(Shared<THREADS> &sh, const u64 *hist, u64 goal, int &bin, u64 &above)
+template <int THREADS> __device__ __forceinline__ u64 find_bin(Shared<THREADS> &sh, const u64 *hist, u64 goal, int &bin, u64 &above)
 {
     constexpr int B = kBins / THREADS;
     u64 own[B], sum = 0;
@@ -180,7 +180,7 @@ template <bool BF16, int THREADS> struct Steps {
     }
     // The first histogram: equal steps from the largest logit down to `lo` and all below it; measure(key, index): what a logit counts
     // (0: nothing).  Returns the total.
-    template <typename M> __device__ u64 first(float m, float lo, M measure)
+    template <typename M> __device__ __forceinline__ u64 first(float m, float lo, M measure)
     {
         hi = m;
         scale = fminf((float)(kBins - 1) / (m - lo), 1e30f);
@@ -201,7 +201,7 @@ template <bool BF16, int THREADS> struct Steps {
         return (int)fminf(fmaxf((hi - value_of(key)) * scale, 0.f), (float)(kBins - 1));
     }
     // The spot at which what `measure` counts, as in the first histogram, reaches `goal` (1 <= goal <= total)
-    template <typename M> __device__ Spot find(u64 goal, M measure) const
+    template <typename M> __device__ __forceinline__ Spot find(u64 goal, M measure) const
     {
         int bin;
         u64 above;
@@ -248,7 +248,7 @@ template <bool BF16, int THREADS> struct Steps {
         }
     }
     // the spot among the `count` <= kFew entries listed
-    template <typename M> __device__ Spot among(u64 goal, u64 above, int count, M measure) const
+    template <typename M> __device__ __forceinline__ Spot among(u64 goal, u64 above, int count, M measure) const
     {
         sort_few(count);
         u64 x = 0, own = 0;
@@ -288,7 +288,7 @@ template <bool BF16, int THREADS> struct Steps {
         __syncthreads();
     }
     // the index of the q-th lowest (from 1) of the logits of one key
-    __device__ int locate(uint32_t key, uint32_t q) const
+    __device__ __forceinline__ int locate(uint32_t key, uint32_t q) const
     {
         int lo = 0, width = row.n;  // the indices in question
         for (;;) {
@@ -337,7 +337,7 @@ struct Params {
         min_p = uniform(p.min_p ? p.min_p[i] : 0.0f);
         min_p = min_p > 0.0f ? fminf(min_p, 1.0f) : 0.0f;
         greedy = !(T > 0.0f) || k == 1;
-        if (k <= 0 || k >= p.r.vocab) k = 0;
+        if (k <= 0 || k >= p.r.vocab || greedy) k = 0;
     }
 };
 
@@ -352,13 +352,17 @@ __device__ __forceinline__ Weight weight_of(float m, float T, int vocab)
     return w;
 }
 
-// Token and its log probability by steps: every row, whatever its logits.
+// Puts the list in order (below)
+template <int THREADS> __device__ __forceinline__ bool sort_list(Shared<THREADS> &sh, int count);
+
+// Token and its log probability by steps: every row, whatever its logits.  m: the largest logit, if known (NaN: not)
 template <bool BF16, int THREADS>
-__device__ void sample_by_steps(Shared<THREADS> &sh, const Row<BF16> &row, const Params &par, float u, int &token, float &logprob)
+__device__ __forceinline__ void sample_by_steps(Shared<THREADS> &sh, const Row<BF16> &row, const Params &par, float u, float m, int &token, float &logprob)
 {
+    constexpr int N = kList / THREADS;
     Steps<BF16, THREADS> steps(sh, row);
-    float m, least;
-    steps.extremes(m, least);
+    float least = kLow;
+    if (!(m == m) || par.k) steps.extremes(m, least);
     token = -1;
     logprob = kNegInf;
     if (!(m > kNegInf)) return;  // (the same for the whole block, as is every choice below)
@@ -380,36 +384,131 @@ __device__ void sample_by_steps(Shared<THREADS> &sh, const Row<BF16> &row, const
         key_min = key_of(f) + ((double)f < low ? 1 : 0);
     }
     u64 over = 0;
-    const u64 total = steps.first(m, fmaxf(least, m - 44.0f * par.T), [&](uint32_t key, int idx) {
+    const float end = fmaxf(least, m - 44.0f * par.T);
+    const u64 total = steps.first(m, end, [&](uint32_t key, int idx) {
         const u64 x = inside(key, idx);
         if (key >= key_min) over += x;
         return x;
     });
-    u64 kept = total;
+    if (key_min) over = block_reduce<u64, THREADS>(over, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
+    else over = total;
+    const double p_goal = ceil((double)par.top_p * (double)total);
+    const u64 cut_goal = !(p_goal >= 1.0) ? 1 : p_goal >= (double)total ? total : (u64)p_goal;
+    auto draw_goal = [&](u64 kept) {
+        const double goal = floor((double)u * (double)kept);
+        return !(goal >= 0.0) ? (u64)1 : goal >= (double)(kept - 1) ? kept : (u64)goal + 1;
+    };
+    // The step of top-p's cut says what is kept but for that step's own weights, and so, nearly always, the step of the draw: both are
+    // listed in one pass, and in order.
+    int cut_bin = -1, bin_1, bin_2;
+    u64 cut_above = 0, above_1, above_2, least_kept = over, most_kept = over;
     if (par.top_p < 1.0f) {
-        const double goal = ceil((double)par.top_p * (double)total);
-        const u64 g = !(goal >= 1.0) ? 1 : goal >= (double)total ? total : (u64)goal;
-        const Spot end = steps.find(g, inside);
-        kept = end.above + w(key_in(end.at));
+        find_bin<THREADS>(sh, sh.hist[0], cut_goal, cut_bin, cut_above);
+        const u64 with = cut_above + sh.hist[0][cut_bin];
+        least_kept = cut_above + 1 < over ? cut_above + 1 : over;
+        most_kept = with < over ? with : over;
+        if (least_kept == most_kept) cut_bin = -1;  // (min-p cuts before)
     }
-    if (key_min) {
-        // (both keep a prefix of the order: the shorter one counts)
-        over = block_reduce<u64, THREADS>(over, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
-        kept = over < kept ? over : kept;
+    find_bin<THREADS>(sh, sh.hist[0], draw_goal(least_kept), bin_1, above_1);
+    find_bin<THREADS>(sh, sh.hist[0], draw_goal(most_kept), bin_2, above_2);
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    steps.each([&](uint32_t key, int idx) {
+        if (key <= kKeyNone) return;
+        const int b = steps.step(key);
+        if ((b < bin_1 || b > bin_2) && b != cut_bin) return;
+        if (!inside(key, idx)) return;
+        const int to = atomicAdd(&sh.count, 1);
+        if (to < kList) sh.listed[to] = entry(key, idx);
+    });
+    __syncthreads();
+    const int count = (int)uniform((uint32_t)sh.count);
+    if (count <= kList && sort_list<THREADS>(sh, count)) {
+        const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+        u64 own[N], sum = 0, sum_draw = 0;
+        int bin[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int e = threadIdx.x * N + n;
+            own[n] = 0;
+            bin[n] = -2;
+            if (e < count) {
+                own[n] = w(key_in(sh.listed[e]));
+                bin[n] = steps.step(key_in(sh.listed[e]));
+            }
+            sum += own[n];
+            if (bin[n] <= bin_2) sum_draw += own[n];
+        }
+        u64 incl = sum;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const u64 up = __shfl_up(incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == kWave - 1) sh.wave_sum[wave] = incl;
+        __syncthreads();
+        for (int k = 0; k < wave; ++k) incl += sh.wave_sum[k];
+        __syncthreads();
+        const u64 draws = block_reduce<u64, THREADS>(sum_draw, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
+        // the running sum in front of an entry: those of the cut's step alone begin at cut_above
+        auto entries = [&](auto f) {
+            u64 run = incl - sum;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                f(n, bin[n] <= bin_2 ? above_1 + run : cut_above + (run - draws));
+                run += own[n];
+            }
+        };
+        u64 kept = over;
+        if (cut_bin >= 0) {
+            entries([&](int n, u64 before) {
+                if (bin[n] == cut_bin && before < cut_goal && cut_goal <= before + own[n]) sh.kept = before + own[n];
+            });
+            __syncthreads();
+            kept = uniform(sh.kept);
+            kept = kept < over ? kept : over;
+        } else if (par.top_p < 1.0f) {
+            kept = least_kept;
+        }
+        const u64 g = draw_goal(kept);
+        entries([&](int n, u64 before) {
+            if (bin[n] >= bin_1 && bin[n] <= bin_2 && before < g && g <= before + own[n]) sh.found = sh.listed[threadIdx.x * N + n];
+        });
+        __syncthreads();
+        const u64 drawn = uniform(sh.found);
+        token = index_in(drawn);
+        logprob = (float)((w.top_inf ? 0.0 : w.log2_of(key_in(drawn)) * 0.69314718055994530942) - log(__builtin_ldexp((double)kept, -w.scale)));
+        return;
     }
-    const double goal = floor((double)u * (double)kept);
-    const u64 g = !(goal >= 0.0) ? 1 : goal >= (double)(kept - 1) ? kept : (u64)goal + 1;
-    const u64 drawn = steps.find(g, inside).at;
+    // too many logits in a step: step by step
+    __syncthreads();
+    steps.first(m, end, inside);
+    u64 kept = over;
+    if (par.top_p < 1.0f) {
+        const Spot cut = steps.find(cut_goal, inside);
+        const u64 with = cut.above + w(key_in(cut.at));
+        kept = with < over ? with : over;
+    }
+    const u64 drawn = steps.find(draw_goal(kept), inside).at;
     token = index_in(drawn);
     logprob = (float)((w.top_inf ? 0.0 : w.log2_of(key_in(drawn)) * 0.69314718055994530942) - log(__builtin_ldexp((double)kept, -w.scale)));
 }
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 halves(uint32_t w) { return __builtin_bit_cast(u16x2, w); }
+
 // The index of the q-th lowest (from 1) of the logits whose bf16 bits are `bits` (not a zero's): counted by runs of 128 chunks,
 // then within the run.
-template <int THREADS> __device__ int locate_bits(Shared<THREADS> &sh, const Row<true> &row, uint32_t bits, uint32_t q)
+template <int THREADS> __device__ __forceinline__ int locate_bits(Shared<THREADS> &sh, const Row<true> &row, uint32_t bits, uint32_t q)
 {
     constexpr int U = 4, kRun = 2 * kWave;
     const int lane = threadIdx.x & (kWave - 1), runs = (row.whole + kRun - 1) / kRun;
+    const u16x2 both = {(uint16_t)bits, (uint16_t)bits};
+    auto any_in_chunk = [&](const uint4 &v) {
+        const u16x2 none = __builtin_elementwise_min(__builtin_elementwise_min(halves(v.x) ^ both, halves(v.y) ^ both),
+                                                     __builtin_elementwise_min(halves(v.z) ^ both, halves(v.w) ^ both));
+        return none.x == 0 || none.y == 0;
+    };
     auto in_chunk = [&](const uint4 &v) {  // one bit an element
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
         uint32_t m = 0;
@@ -431,10 +530,7 @@ template <int THREADS> __device__ int locate_bits(Shared<THREADS> &sh, const Row
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = c + u * THREADS;
-            if (at < row.whole) {
-                const uint32_t m = in_chunk(v[u]);
-                if (m) atomicAdd(&hist[1 + at / kRun], (u64)__popc(m));
-            }
+            if (at < row.whole && any_in_chunk(v[u])) atomicAdd(&hist[1 + at / kRun], (u64)__popc(in_chunk(v[u])));
             v[u] = load_chunk<false>(from, at + U * THREADS);
         }
     }
@@ -470,47 +566,33 @@ template <int THREADS> __device__ int locate_bits(Shared<THREADS> &sh, const Row
     return found;
 }
 
-// Token and log probability of a row of bf16 by counting how often each logit occurs; false: not that kind of row (a largest logit far beyond
-// those of the row's first round, NaN among the logits, many near 0).
-//   slots 0 .. 2047: positive logits, falling; 2048: those nearer to 0 than any slot, listed; 2049 ..: negative ones
+// Token and log probability of a row of bf16 by counting how often each logit occurs; false: not that kind of row (NaN, infinity or a
+// logit from 2^17 on among its logits, or many near 0).
+//   slot t + kSlots / 2 (if negative): magnitude kNearest + t in bf16 bits.  In the order of the row: positive logits, t falling; those nearer to 0 than any
+//   slot, listed; negative ones, t rising
 template <int THREADS>
-__device__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const Params &par, float u, int &token, float &logprob)
+__device__ __forceinline__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const Params &par, float u, int &token, float &logprob)
 {
-    constexpr int U = 4, N = kSlots / THREADS, W = THREADS / kWave, kZero = 2048;
+    constexpr int U = 4, N = kSlots / THREADS, W = THREADS / kWave, kHalf = kSlots / 2, kMiddle = kHalf / N;
+    constexpr uint32_t kNearest = 0x3800u;  // 2^-15
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const __amdgpu_buffer_rsrc_t from = row.buffer();
     uint4 v[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) v[k] = load_chunk<false>(from, k * THREADS + threadIdx.x);
-    const float edge_z = row.edge(threadIdx.x);
-    for (int k = threadIdx.x; k < kSlots; k += THREADS) sh.times[k] = 0;
-    if (threadIdx.x == 0) {
-        sh.count = 0;
-        sh.queued = 0;
-    }
-    float top = fmaxf(edge_z, kNegInf);
-#pragma unroll
-    for (int k = 0; k < U; ++k)
-        if (k * THREADS + (int)threadIdx.x < row.whole) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, Row<true>::value(v[k], e));
-        }
-    top = block_max<THREADS>(top, sh.red);
-    if (!(top > kNegInf)) return false;
-    // 16 octaves: the uppermost above that of the first round's largest logit and of what weighs nothing beside it
-    const float reach = fmaxf(fabsf(top), fminf(fabsf(top - 44.0f * par.T), 3e38f));
-    const int last = (int)((__float_as_uint(reach) >> 16) | 0x7fu) + 0x80;  // greatest magnitude with a slot, in bf16 bits
-    const int base = last - 2047;                                          // least
-    if (last >= 0x7f80 || base <= 0) return false;
+    for (int k = threadIdx.x; k < kSlots / 4; k += THREADS) ((uint4 *)sh.times)[k] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x == 0) sh.count = sh.queued = 0;
+    __syncthreads();
+    // a logit that may have no slot
     auto count = [&](uint32_t h, int idx) {
-        const int mag = (int)(h & 0x7fffu) - base;
-        if ((uint32_t)mag < 2047u + (h < 0x8000u ? 1u : 0u)) {
-            atomicAdd(&sh.times[h < 0x8000u ? 2047 - mag : 2049 + mag], 1u);
-        } else if (mag < 0) {
+        const uint32_t mag = h & 0x7fffu, t = mag - kNearest;
+        if (t < (uint32_t)kHalf) {
+            atomicAdd(&sh.times[t + (h >> 15) * kHalf], 1u);
+        } else if (mag < kNearest) {
             const int to = atomicAdd(&sh.count, 1);
             if (to < kFew) sh.listed[to] = entry(key_of(bf16_to_f32(h)), idx);
-        } else if (h < 0x8000u || h > 0xff80u) {
-            sh.queued = 1;  // beyond the slots, or NaN
+        } else if (h != 0xff80u) {
+            sh.queued = 1;
         }
     };
     if ((int)threadIdx.x < row.edges) count(((const uint16_t *)row.row)[row.edge_index(threadIdx.x)], row.edge_index(threadIdx.x));
@@ -520,8 +602,26 @@ __device__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const
             const int at = c + k * THREADS;
             if (at < row.whole) {
                 const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+                // two logits at a time: the bits less kNearest have a slot where bits 12 to 14 are clear
+                u16x2 x[4];
+                uint32_t out = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) count((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu, row.lo + at * 8 + e);
+                for (int j = 0; j < 4; ++j) {
+                    x[j] = halves(w[j]) - u16x2{(uint16_t)kNearest, (uint16_t)kNearest};
+                    out |= __builtin_bit_cast(uint32_t, x[j]) & 0x70007000u;
+                }
+                if (!out) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const u16x2 sign = x[j] >> u16x2{15, 15};
+                        const uint32_t to = __builtin_bit_cast(uint32_t, (u16x2)((x[j] << u16x2{2, 2}) + sign * u16x2{4 * kHalf, 4 * kHalf}));  // in bytes
+                        atomicAdd((uint32_t *)((char *)sh.times + (to & 0xffffu)), 1u);
+                        atomicAdd((uint32_t *)((char *)sh.times + (to >> 16)), 1u);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) count((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu, row.lo + at * 8 + e);
+                }
             }
             v[k] = load_chunk<false>(from, at + U * THREADS);
         }
@@ -530,30 +630,25 @@ __device__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const
     const int near_zero = (int)uniform((uint32_t)sh.count);
     if (uniform((uint32_t)sh.queued) || near_zero > kFew) return false;
     if (near_zero) Steps<true, THREADS>(sh, row).sort_few(near_zero);
-    // thread t has slots N t .. N t + N - 1
-    uint32_t times[N];
-    int first = kSlots;
+    // thread t has slots N t .. N t + N - 1 in the order of the row; the logits near 0 are in front of thread kMiddle's
+    auto slot_at = [&](int o) { return o < kHalf ? kHalf - 1 - o : o; };
+    auto key_at = [&](int o) { return key_of(bf16_to_f32(o < kHalf ? kNearest + (kHalf - 1 - o) : 0x8000u + kNearest + (o - kHalf))); };
+    int first = kSlots, own = 0;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const int slot = threadIdx.x * N + n;
-        times[n] = slot == kZero ? (uint32_t)near_zero : sh.times[slot];
-        if (times[n] && first == kSlots) first = slot;
+    for (int n = N - 1; n >= 0; --n) {
+        const int o = threadIdx.x * N + n, times = (int)sh.times[slot_at(o)];
+        if (times) first = o;
+        own += times;
     }
-    first = (int)-block_max<THREADS>((float)-first, sh.red);  // of the largest logit
-    auto key_at = [&](int slot) {  // (not of kZero)
-        const uint32_t h = slot < kZero ? (uint32_t)(base + 2047 - slot) : 0x8000u | (uint32_t)(base + slot - 2049);
-        return key_of(bf16_to_f32(h));
-    };
+    first = (int)-block_max<THREADS>((float)-first, sh.red);  // of the largest logit, but for those near 0
     const u64 *zeros = sh.listed + kFew;
-    if (first == kSlots) return false;
-    const float m = first == kZero ? value_in(zeros[0]) : value_of(key_at(first));
+    if (first == kSlots && !near_zero) return false;
+    const float m = near_zero && first >= kHalf ? value_in(zeros[0]) : value_of(key_at(first));
     const Weight w = weight_of(m, par.T, row.n);
+    int zeros_kept = near_zero;
     // how many the top-k keeps of each slot
     if (par.k) {
-        int incl = 0, own = 0;
-#pragma unroll
-        for (int n = 0; n < N; ++n) own += (int)times[n];
-        incl = own;
+        int incl = own;
 #pragma unroll
         for (int o = 1; o < kWave; o <<= 1) {
             const int up = __shfl_up(incl, o);
@@ -561,50 +656,53 @@ __device__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const
         }
         if (lane == kWave - 1) sh.wave_sum[wave] = (u64)incl;
         __syncthreads();
-        int run = incl - own, all = 0;
+        int run = incl - own, all = near_zero;
         for (int k = 0; k < W; ++k) {
             if (k < wave) run += (int)sh.wave_sum[k];
             all += (int)sh.wave_sum[k];
         }
+        if (threadIdx.x == kMiddle) sh.cut_m = run >= par.k ? 0 : par.k - run < near_zero ? par.k - run : near_zero;
         __syncthreads();
-        if (all < par.k) return false;  // (some may lie below the slots)
+        zeros_kept = (int)uniform((uint32_t)sh.cut_m);
+        if (all < par.k) return false;  // (what is beyond the slots may be asked for)
+        if (threadIdx.x >= kMiddle) run += near_zero;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
+            uint32_t &times = sh.times[slot_at(threadIdx.x * N + n)];
             const int left = par.k - run;
-            run += (int)times[n];
-            times[n] = left <= 0 ? 0 : (uint32_t)left < times[n] ? (uint32_t)left : times[n];
+            run += (int)times;
+            if (left < (int)times) times = left > 0 ? (uint32_t)left : 0;
         }
     }
     // weights, and those that min-p keeps
     double low = kNegInf;
     if (par.min_p > 0.0f) low = w.m + (double)par.T * log((double)par.min_p);
-    u64 one[N], own[N], sum = 0, over = 0, of_zeros = 0;
+    u64 sum = 0, over = 0, of_zeros = 0;
     u64 *const weight_of_zero = sh.listed + 2 * kFew;
     if (near_zero) {
-        if (threadIdx.x == kZero / N) sh.cut_m = (int)times[kZero % N];
-        __syncthreads();
         u64 x = 0;
-        if ((int)threadIdx.x < sh.cut_m) {
+        if ((int)threadIdx.x < zeros_kept) {
             x = w(key_in(zeros[threadIdx.x]));
             if ((double)value_in(zeros[threadIdx.x]) >= low) over = x;
             weight_of_zero[threadIdx.x] = x;
         }
         of_zeros = block_reduce<u64, THREADS>(x, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
     }
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const int slot = threadIdx.x * N + n;
-        one[n] = own[n] = 0;
-        if (!times[n]) continue;
-        if (slot == kZero) {
-            own[n] = of_zeros;
-        } else {
-            one[n] = w(key_at(slot));
-            own[n] = one[n] * times[n];
-            if ((double)value_of(key_at(slot)) >= low) over += own[n];
+    // f(weight of the slots so far, of one logit of this slot, how many, its place in the order) over the thread's slots that occur
+    auto each_slot = [&](u64 run, auto f) {
+#pragma nounroll
+        for (int o = threadIdx.x * N; o < (int)threadIdx.x * N + N; ++o) {
+            const uint32_t times = sh.times[slot_at(o)];
+            if (!times) continue;
+            const u64 one = w(key_at(o));
+            f(run, one, times, o);
+            run += one * times;
         }
-        sum += own[n];
-    }
+        return run;
+    };
+    sum = each_slot(0, [&](u64, u64 one, uint32_t times, int o) {
+        if ((double)value_of(key_at(o)) >= low) over += one * times;
+    });
     u64 incl = sum;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
@@ -620,29 +718,27 @@ __device__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const
         total += sh.wave_sum[k];
     }
     __syncthreads();
+    total += of_zeros;
+    if (threadIdx.x >= kMiddle) incl += of_zeros;
     const u64 begin = incl - sum;
-    // where the running sum reaches `goal`: the slot, how many of it (from 1), and the sum with those
+    // where the running sum reaches `goal`: the slot (kSlots: near 0), how many of it (from 1), and the sum with those
     auto find = [&](u64 goal, int &slot, uint32_t &q, u64 &with) {
         if (goal > begin && goal <= incl) {
-            u64 run = begin;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                if (goal > run && goal <= run + own[n]) {
-                    const int at = threadIdx.x * N + n;
-                    uint32_t many = 0;
-                    u64 x = run;
-                    if (at == kZero) {
-                        while (x < goal) x += weight_of_zero[many++];
-                    } else {
-                        many = (uint32_t)((goal - run + one[n] - 1) / one[n]);
-                        x += many * one[n];
-                    }
-                    sh.bin = at;
-                    sh.drawn = (int)many;
-                    sh.above = x;
-                }
-                run += own[n];
-            }
+            each_slot(begin, [&](u64 run, u64 one, uint32_t times, int o) {
+                if (goal <= run || goal > run + one * times) return;
+                const uint32_t many = (uint32_t)((goal - run + one - 1) / one);
+                sh.bin = o;
+                sh.drawn = (int)many;
+                sh.above = run + many * one;
+            });
+        }
+        if (threadIdx.x == kMiddle && goal <= begin && goal > begin - of_zeros) {
+            u64 x = begin - of_zeros;
+            int many = 0;
+            while (x < goal) x += weight_of_zero[many++];
+            sh.bin = kSlots;
+            sh.drawn = many;
+            sh.above = x;
         }
         __syncthreads();
         slot = (int)uniform((uint32_t)sh.bin);
@@ -665,7 +761,7 @@ __device__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const
     const double goal = floor((double)u * (double)kept);
     find(!(goal >= 0.0) ? 1 : goal >= (double)(kept - 1) ? kept : (u64)goal + 1, slot, q, with);
     uint32_t key;
-    if (slot == kZero) {
+    if (slot == kSlots) {
         key = key_in(zeros[q - 1]);
         token = index_in(zeros[q - 1]);
     } else {
@@ -681,7 +777,7 @@ struct Found {
     int count;    // listed
     bool whole;   // every logit above -inf is listed
     double rest;  // sum of exp((z - ref) / T) over what is not listed
-    float ref;
+    float ref, top;  // what the sum is relative to; the largest logit
     bool ok;      // the list is not too long (and what it is sorted by is a number)
     bool summed;  // `rest` is right but for 2^-17 of it
 };
@@ -701,7 +797,7 @@ __device__ __forceinline__ uint32_t rank_in_wave(float v, int rank)
 
 // Lists the beginning of the row, at least `want` logits where there are as many, and sums the rest (if `sums`).  Chunks with a logit to
 // list are put aside, for a thread each to look at later: among the others the pass does not branch.
-template <bool BF16, int THREADS> __device__ Found list_row(Shared<THREADS> &sh, const Row<BF16> &row, int want, bool sums, float tau)
+template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shared<THREADS> &sh, const Row<BF16> &row, int want, bool sums, float tau)
 {
     constexpr int E = Row<BF16>::E, U = 4, W = THREADS / kWave, kRound = U * THREADS;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -766,8 +862,13 @@ template <bool BF16, int THREADS> __device__ Found list_row(Shared<THREADS> &sh,
             v[u] = load_chunk<false>(from, at + kRound);
         }
     }
+    {
+        const float m = wave_max(top);
+        if (lane == 0) sh.all[wave] = m;
+    }
     if (r > 1) raise_bound(r);
     else __syncthreads();
+    const float largest_logit = uniform(wave_max(sh.all[lane & (W - 1)]));
     // everything from the last bound on is listed
     auto look_at = [&](float z, int idx) {
         if (z >= bound) {
@@ -791,6 +892,7 @@ template <bool BF16, int THREADS> __device__ Found list_row(Shared<THREADS> &sh,
     f.count = (int)uniform((uint32_t)sh.count);
     f.whole = bound == kLow;
     f.ref = by_T.ref;
+    f.top = largest_logit;
     f.rest = rest * exp2_neg(-by_T.drift(), 0);
     f.ok = f.count <= kList && queued <= kQueue;
     f.summed = rest < 1e30 && fabs(by_T.drift() - 32.0) < 1.0;
@@ -798,7 +900,7 @@ template <bool BF16, int THREADS> __device__ Found list_row(Shared<THREADS> &sh,
 }
 
 // Puts the list in order: a counting sort by equal steps of the logit, then each entry behind those of its step that are before it.
-template <int THREADS> __device__ bool sort_list(Shared<THREADS> &sh, int count)
+template <int THREADS> __device__ __forceinline__ bool sort_list(Shared<THREADS> &sh, int count)
 {
     constexpr int W = THREADS / kWave, N = kList / THREADS, B = kSteps / THREADS;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -894,6 +996,7 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
         if (!par.greedy && (!par.k || par.k > kMost)) done = sample_by_slots<THREADS>(sh, row, par, u, token, logprob);
     Found f;
     f.ok = false;
+    f.top = __builtin_nanf("");
     if (!done && want <= kMost) {
         if (BF16 && sums) __syncthreads();
         f = list_row<BF16, THREADS>(sh, row, want, sums, par.greedy ? 1.0f : par.T);
@@ -999,7 +1102,7 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     }
     if (!done) {
         __syncthreads();
-        sample_by_steps<BF16, THREADS>(sh, row, par, u, token, logprob);
+        sample_by_steps<BF16, THREADS>(sh, row, par, u, f.top, token, logprob);
     }
     if (threadIdx.x == 0) {
         p.token[i] = token;
