@@ -41,6 +41,7 @@ constexpr int kList = 4096;                 // logits listed of a row
 constexpr int kSteps = 1024;                // of the logit, in the counting sort
 constexpr int kQueue = 1536;                // chunks with logits to list
 constexpr int kMost = 256;                  // logits that a row is asked to list
+constexpr int kShort = 192;                  // entries of a list that is put in order without steps
 constexpr int kFew = 512;                   // logits of one step that are listed
 
 // bits that rise with the value; NaN counts as -inf, -0 as 0
@@ -91,53 +92,82 @@ template <int THREADS> struct Shared {
     u64 wave_sum[THREADS / kWave];
     double red[THREADS / kWave];
     float low[2][THREADS / kWave], top[THREADS / kWave], all[THREADS / kWave];
-    u64 above, found;
+    u64 above, found, aboves[2];
+    int bins[2];
     uint32_t key_min, key_max;
     int bin;
     int count, queued;
-    int cut_p[2], cut_m, drawn;
+    int cut_m, drawn;
+    float logprob;
     u64 kept;
 };
 
-// The first bin at which the running sum over the bins reaches `goal` (1 <= goal <= total), and the sum before it;
-// returns the total.  goal 0: the total alone.
-template <int THREADS> __device__ __forceinline__ u64 find_bin(Shared<THREADS> &sh, const u64 *hist, u64 goal, int &bin, u64 &above)
-{
-    constexpr int B = kBins / THREADS;
-    u64 own[B], sum = 0;
+// A histogram's running sum: thread t has bins B t .. B t + B - 1
+template <int THREADS> struct Scan {
+    static constexpr int B = kBins / THREADS;
+    u64 begin, end, total;
+    __device__ __forceinline__ Scan() {}
+    __device__ __forceinline__ Scan(Shared<THREADS> &sh, const u64 *hist)
+    {
+        u64 sum = 0;
 #pragma unroll
-    for (int b = 0; b < B; ++b) sum += own[b] = hist[threadIdx.x * B + b];
-    u64 incl = sum;
-    const int lane = threadIdx.x & (kWave - 1);
+        for (int b = 0; b < B; ++b) sum += hist[threadIdx.x * B + b];
+        end = sum;
+        const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const u64 up = __shfl_up(incl, o);
-        if (lane >= o) incl += up;
-    }
-    if (lane == kWave - 1) sh.wave_sum[threadIdx.x / kWave] = incl;
-    __syncthreads();
-    u64 total = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / kWave; ++w) {
-        if (w == (int)(threadIdx.x / kWave)) incl += total;
-        total += sh.wave_sum[w];
-    }
-    u64 run = incl - sum;
-    if (goal > run && goal <= incl) {
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-            if (goal > run && goal <= run + own[b]) {
-                sh.bin = threadIdx.x * B + b;
-                sh.above = run;
-            }
-            run += own[b];
+        for (int o = 1; o < kWave; o <<= 1) {
+            const u64 up = __shfl_up(end, o);
+            if (lane >= o) end += up;
         }
+        if (lane == kWave - 1) sh.wave_sum[threadIdx.x / kWave] = end;
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / kWave; ++w) {
+            if (w == (int)(threadIdx.x / kWave)) end += total;
+            total += sh.wave_sum[w];
+        }
+        begin = end - sum;
+        total = uniform(total);
+        __syncthreads();
     }
-    __syncthreads();
-    bin = sh.bin;
-    above = sh.above;
-    __syncthreads();
-    return total;
+    // The first bins at which the running sum reaches goal[0] and goal[1] (1 <= goal <= total), and the sums before them
+    __device__ __forceinline__ void find(Shared<THREADS> &sh, const u64 *hist, const u64 (&goal)[2], int (&bin)[2], u64 (&above)[2]) const
+    {
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            if (goal[a] <= begin || goal[a] > end) continue;
+            u64 run = begin;
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const u64 own = hist[threadIdx.x * B + b];
+                if (goal[a] > run && goal[a] <= run + own) {
+                    sh.bins[a] = threadIdx.x * B + b;
+                    sh.aboves[a] = run;
+                }
+                run += own;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            bin[a] = (int)uniform((uint32_t)sh.bins[a]);
+            above[a] = uniform(sh.aboves[a]);
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ void find(Shared<THREADS> &sh, const u64 *hist, u64 goal, int &bin, u64 &above) const
+    {
+        int b[2];
+        u64 a[2];
+        find(sh, hist, {goal, 0}, b, a);
+        bin = b[0];
+        above = a[0];
+    }
+};
+template <int THREADS> __device__ __forceinline__ void find_bin(Shared<THREADS> &sh, const u64 *hist, u64 goal, int &bin, u64 &above)
+{
+    Scan<THREADS>(sh, hist).find(sh, hist, goal, bin, above);
 }
 
 // What is found by steps: the entry at which a running sum over the order of the row reaches a goal, and the sum before it
@@ -148,7 +178,8 @@ struct Spot {
 template <bool BF16, int THREADS> struct Steps {
     Shared<THREADS> &sh;
     const Row<BF16> row;
-    float hi, scale;  // the first histogram's steps
+    float hi, scale;      // the first histogram's steps
+    Scan<THREADS> scan;  // and its running sum
 
     __device__ __forceinline__ Steps(Shared<THREADS> &s, const Row<BF16> &r) : sh(s), row(r) {}
 
@@ -192,9 +223,8 @@ template <bool BF16, int THREADS> struct Steps {
             if (x) atomicAdd(&sh.hist[0][step(key)], x);
         });
         __syncthreads();
-        int bin;
-        u64 above;
-        return find_bin<THREADS>(sh, sh.hist[0], 0, bin, above);
+        scan = Scan<THREADS>(sh, sh.hist[0]);
+        return scan.total;
     }
     __device__ __forceinline__ int step(uint32_t key) const
     {
@@ -205,7 +235,7 @@ template <bool BF16, int THREADS> struct Steps {
     {
         int bin;
         u64 above;
-        find_bin<THREADS>(sh, sh.hist[0], goal, bin, above);
+        scan.find(sh, sh.hist[0], goal, bin, above);
         uint32_t k_lo = kKeyNone + 1, k_hi = 0xffffffffu;  // the keys in question
         int shift = -1;                                    // steps of their bits (-1: those of the first histogram)
         for (;;) {
@@ -400,24 +430,26 @@ __device__ __forceinline__ void sample_by_steps(Shared<THREADS> &sh, const Row<B
     };
     // The step of top-p's cut says what is kept but for that step's own weights, and so, nearly always, the step of the draw: both are
     // listed in one pass, and in order.
-    int cut_bin = -1, bin_1, bin_2;
-    u64 cut_above = 0, above_1, above_2, least_kept = over, most_kept = over;
+    int cut_bin = -1;
+    u64 cut_above = 0, least_kept = over, most_kept = over;
     if (par.top_p < 1.0f) {
-        find_bin<THREADS>(sh, sh.hist[0], cut_goal, cut_bin, cut_above);
-        const u64 with = cut_above + sh.hist[0][cut_bin];
+        steps.scan.find(sh, sh.hist[0], cut_goal, cut_bin, cut_above);
+        const u64 with = cut_above + uniform(sh.hist[0][cut_bin]);
         least_kept = cut_above + 1 < over ? cut_above + 1 : over;
         most_kept = with < over ? with : over;
         if (least_kept == most_kept) cut_bin = -1;  // (min-p cuts before)
     }
-    find_bin<THREADS>(sh, sh.hist[0], draw_goal(least_kept), bin_1, above_1);
-    find_bin<THREADS>(sh, sh.hist[0], draw_goal(most_kept), bin_2, above_2);
+    int draw_bin[2];
+    u64 draw_above[2];
+    steps.scan.find(sh, sh.hist[0], {draw_goal(least_kept), draw_goal(most_kept)}, draw_bin, draw_above);
+    const int bin_1 = draw_bin[0], bin_2 = draw_bin[1];
+    const u64 above_1 = draw_above[0];
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     steps.each([&](uint32_t key, int idx) {
         if (key <= kKeyNone) return;
         const int b = steps.step(key);
-        if ((b < bin_1 || b > bin_2) && b != cut_bin) return;
-        if (!inside(key, idx)) return;
+        if (((b < bin_1 || b > bin_2) && b != cut_bin) || entry(key, idx) > last) return;
         const int to = atomicAdd(&sh.count, 1);
         if (to < kList) sh.listed[to] = entry(key, idx);
     });
@@ -519,22 +551,32 @@ template <int THREADS> __device__ __forceinline__ int locate_bits(Shared<THREADS
     // bins: the edges in front, the runs, the edges behind
     u64 *const hist = sh.hist[0];
     for (int r = threadIdx.x; r < kBins; r += THREADS) hist[r] = 0;
+    if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     const bool at_edge = (int)threadIdx.x < row.edges && ((const uint16_t *)row.row)[row.edge_index(threadIdx.x)] == (uint16_t)bits;
     if (at_edge) atomicAdd(&hist[(int)threadIdx.x < row.lo ? 0 : 1 + runs], (u64)1);
+    if (at_edge && (int)threadIdx.x < row.lo) atomicAdd(&sh.count, 1);
     const __amdgpu_buffer_rsrc_t from = row.buffer();
     uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = load_chunk<false>(from, u * THREADS + threadIdx.x);
-    for (int c = threadIdx.x; c < row.whole; c += U * THREADS) {
+    // (as far as the q-th: half the row, on average)
+    for (int c = threadIdx.x, done = 0; done < row.whole; c += U * THREADS, done += U * THREADS) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = c + u * THREADS;
-            if (at < row.whole && any_in_chunk(v[u])) atomicAdd(&hist[1 + at / kRun], (u64)__popc(in_chunk(v[u])));
+            if (at < row.whole && any_in_chunk(v[u])) {
+                const int n = __popc(in_chunk(v[u]));
+                atomicAdd(&hist[1 + at / kRun], (u64)n);
+                atomicAdd(&sh.count, n);
+            }
             v[u] = load_chunk<false>(from, at + U * THREADS);
         }
+        __syncthreads();
+        const bool met = uniform((uint32_t)sh.count) >= q;
+        __syncthreads();
+        if (met) break;
     }
-    __syncthreads();
     int bin;
     u64 above;
     find_bin<THREADS>(sh, hist, q, bin, above);
@@ -899,11 +941,25 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     return f;
 }
 
-// Puts the list in order: a counting sort by equal steps of the logit, then each entry behind those of its step that are before it.
+// Puts the list in order.  A long one: a counting sort by equal steps of the logit, then each entry behind those of its step that are before it.
 template <int THREADS> __device__ __forceinline__ bool sort_list(Shared<THREADS> &sh, int count)
 {
     constexpr int W = THREADS / kWave, N = kList / THREADS, B = kSteps / THREADS;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    if (count <= kShort) {
+        // (a short one: each entry behind those before it)
+        u64 x = 0;
+        int at = 0;
+        if ((int)threadIdx.x < count) {
+            x = sh.listed[threadIdx.x];
+#pragma unroll 8
+            for (int j = 0; j < count; ++j) at += sh.listed[j] < x;
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < count) sh.listed[at] = x;
+        __syncthreads();
+        return true;
+    }
     u64 mine[N];
     float top = kNegInf, low = __builtin_huge_valf();
 #pragma unroll
@@ -976,12 +1032,102 @@ template <int THREADS> __device__ __forceinline__ bool sort_list(Shared<THREADS>
     return true;
 }
 
+// What a list in order says, by one wave: sh.drawn whether it decides the row, sh.bin the token, sh.logprob.  rest: sum of the weights that are
+// not listed, good to 2^-17 of it; whole: there are none.
+template <int THREADS>
+__device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par, float u, const Weight &w, int count, double rest, bool whole)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    // lane l has entries each * l ..; their weights beside them
+    const int n_k = par.k && par.k < count ? par.k : count, each = (n_k + kWave - 1) / kWave;
+    const int begin = lane * each < n_k ? lane * each : n_k, end = begin + each < n_k ? begin + each : n_k;
+    u64 sum = 0;
+#pragma nounroll
+    for (int e = begin; e < end; ++e) {
+        const u64 x = w(key_in(sh.listed[e]));
+        sh.binned[e] = x;
+        sum += x;
+    }
+    u64 incl = sum;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const u64 up = __shfl_up(incl, o);
+        if (lane >= o) incl += up;
+    }
+    const u64 first = incl - sum, listed = uniform((u64)__shfl(incl, kWave - 1));
+    // what all weights sum to, at least and at most
+    const double all[2] = {(double)listed + rest * (1.0 - 0x1p-17), (double)listed + rest * (1.0 + 0x1p-17)};
+    // the first entries that the cuts leave out
+    int cut[2] = {n_k, n_k}, cut_m = n_k;
+    if (par.top_p < 1.0f || par.min_p > 0.0f) {
+        const double low = w.m + (double)par.T * log((double)par.min_p);
+        u64 before = first;
+#pragma nounroll
+        for (int e = begin; e < end; ++e) {
+            if (e > 0 && par.top_p < 1.0f) {
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+                    if (e < cut[a] && (double)before >= (double)par.top_p * all[a]) cut[a] = e;
+            }
+            if (e < cut_m && par.min_p > 0.0f && (double)value_in(sh.listed[e]) < low) cut_m = e;
+            before += sh.binned[e];
+        }
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) {
+            cut[0] = min(cut[0], __shfl_xor(cut[0], o));
+            cut[1] = min(cut[1], __shfl_xor(cut[1], o));
+            cut_m = min(cut_m, __shfl_xor(cut_m, o));
+        }
+    }
+    const int n = cut[0] < cut_m ? cut[0] : cut_m;
+    // the list has to reach the cut: as the end of the top-k, of the row, or because something cuts before its end (for certain)
+    const bool ends = n < n_k || par.k || whole;
+    const bool open = !ends && !(par.top_p < 1.0f) && !(par.min_p > 0.0f);  // nothing cuts at all
+    bool decides = (ends || open) && (cut[0] == cut[1] || n < cut[0]);
+    u64 kept = 0;
+    {
+        u64 before = first;
+#pragma nounroll
+        for (int e = begin; e < end && e < n; ++e) before += sh.binned[e];
+        kept = before - first;
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) kept += __shfl_xor(kept, o);
+        kept = uniform(kept);
+    }
+    // the draw: the first entry whose running sum passes u times the sum, for both ends of what that may be
+    int drawn[2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        const double goal = (double)u * (ends ? (double)kept : all[a]);
+        u64 g = !(goal >= 0.0) ? 0 : (u64)goal;  // (passes: more than that, whole)
+        if (ends && g >= kept) g = kept - 1;
+        int at = -1;
+        if (first <= g && g < incl) {
+            u64 before = first;
+            int e = begin;
+            for (; before + sh.binned[e] <= g; ++e) before += sh.binned[e];
+            at = e;
+        }
+        const u64 who = __ballot(at >= 0);
+        drawn[a] = who ? (int)uniform((uint32_t)__shfl(at, __ffsll(who) - 1)) : -1;
+    }
+    decides = decides && drawn[0] >= 0 && drawn[0] == drawn[1];
+    if (lane == 0) {
+        sh.drawn = decides ? 1 : 0;
+        if (decides) {
+            const u64 x = sh.listed[drawn[0]];
+            const double of = ends ? (double)kept : 0.5 * (all[0] + all[1]);
+            sh.bin = index_in(x);
+            sh.logprob = (float)(w.log2_of(key_in(x)) * 0.69314718055994530942 - log(__builtin_ldexp(of, -w.scale)));
+        }
+    }
+}
+
 // One block a row.  What bounds it: one pass over the row, and the latency of the steps behind it.
 template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) sample_kernel(SampleArgs p)
 {
-    constexpr int N = kList / THREADS, W = THREADS / kWave;
     __shared__ Shared<THREADS> sh;
-    const int i = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int i = blockIdx.x, wave = (int)uniform((uint32_t)threadIdx.x / kWave);
     const void *at = row_of(p.r, i);
     const Row<BF16> row(at, at ? p.r.vocab : 0);
     const Params par(p, i);
@@ -1002,7 +1148,17 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
         f = list_row<BF16, THREADS>(sh, row, want, sums, par.greedy ? 1.0f : par.T);
         done = f.ok && f.count == 0;  // nothing above -inf
     }
-    if (!done && f.ok && (!sums || f.summed) && (!par.k || f.count >= par.k || f.whole) && sort_list<THREADS>(sh, f.count)) {
+    bool reaches = !done && f.ok && (!sums || f.summed) && (!par.k || f.count >= par.k || f.whole);
+    if (reaches && sums && !f.whole) {
+        // (what the list weighs, nearly: a list that cannot reach is not put in order)
+        const Exp by_T(par.T, f.ref);
+        double part = 0.0;
+        for (int e = threadIdx.x; e < f.count; e += THREADS) part += (double)by_T(value_in(sh.listed[e]));
+        part = block_sum<THREADS>(part, sh.red);
+        const float share = par.top_p < 1.0f ? par.top_p : par.min_p > 0.0f ? 0.0f : u;
+        reaches = part * 1.001 >= (double)share * (part + f.rest);
+    }
+    if (reaches && sort_list<THREADS>(sh, f.count)) {
         const float m = value_in(sh.listed[0]);
         if (par.greedy) {
             token = index_in(sh.listed[0]);
@@ -1010,94 +1166,13 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
             done = true;
         } else if (m < __builtin_huge_valf()) {
             const Weight w = weight_of(m, par.T, row.n);
-            // weights of the list, and their running sum; thread t has entries N t .. N t + N - 1
-            const int n_k = par.k && par.k < f.count ? par.k : f.count;
-            u64 own[N], sum = 0;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int e = threadIdx.x * N + n;
-                own[n] = e < n_k ? w(key_in(sh.listed[e])) : 0;
-                sum += own[n];
-            }
-            u64 incl = sum;
-#pragma unroll
-            for (int o = 1; o < kWave; o <<= 1) {
-                const u64 up = __shfl_up(incl, o);
-                if (lane >= o) incl += up;
-            }
-            if (lane == kWave - 1) sh.wave_sum[wave] = incl;
-            if (threadIdx.x == 0) {
-                sh.cut_p[0] = sh.cut_p[1] = sh.cut_m = n_k;
-                sh.drawn = -1;
-            }
-            __syncthreads();
-            u64 listed = 0;
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-                if (j == wave) incl += listed;
-                listed += sh.wave_sum[j];
-            }
-            const u64 first = incl - sum;
-            // what the row's weights sum to, at least and at most
+            // what the row's weights beside the list sum to
             const double rest = sums ? f.rest * exp2_neg(((double)f.ref - (double)m) * w.c, w.scale) : 0.0;
-            const double all[2] = {(double)listed + rest * (1.0 - 0x1p-17), (double)listed + rest * (1.0 + 0x1p-17)};
-            const double low = (double)m + (double)par.T * log((double)par.min_p);
-            if (par.top_p < 1.0f || par.min_p > 0.0f) {
-                u64 before = first;
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const int e = threadIdx.x * N + n;
-                    if (e > 0 && e < n_k) {
-#pragma unroll
-                        for (int a = 0; a < 2; ++a)
-                            if (par.top_p < 1.0f && (double)before >= (double)par.top_p * all[a]) atomicMin(&sh.cut_p[a], e);
-                        if (par.min_p > 0.0f && (double)value_in(sh.listed[e]) < low) atomicMin(&sh.cut_m, e);
-                    }
-                    before += own[n];
-                }
-                __syncthreads();
-            }
-            const int cut_p = sh.cut_p[0], cut_m = sh.cut_m, n = cut_p < cut_m ? cut_p : cut_m;
-            // the list has to reach the cut: as the end of the top-k, of the row, or because something cuts before its end (for certain)
-            const bool ends = n < n_k || par.k || f.whole;
-            const bool open = !ends && !(par.top_p < 1.0f) && !(par.min_p > 0.0f);  // nothing cuts at all
-            if ((ends || open) && (sh.cut_p[0] == sh.cut_p[1] || n < cut_p)) {
-                // the weights kept
-                u64 before = first;
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    before += own[j];
-                    if ((int)threadIdx.x * N + j == n - 1) sh.kept = before;
-                }
-                __syncthreads();
-                const u64 kept = sh.kept;
-                // the draw: the first entry whose running sum passes `goal`, for both ends of what the sum may be
-                int drawn[2];
-#pragma unroll
-                for (int a = 0; a < 2; ++a) {
-                    const double of = ends ? (double)kept : all[a];
-                    const double goal = (double)u * of;
-                    before = first;
-                    if (a == 1) __syncthreads();
-                    u64 g = !(goal >= 0.0) ? 0 : (u64)goal;  // (passes: more than that, whole)
-                    if (ends && g >= kept) g = kept - 1;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        if (before <= g && g < before + own[j]) sh.drawn = threadIdx.x * N + j;
-                        before += own[j];
-                    }
-                    __syncthreads();
-                    drawn[a] = sh.drawn;
-                    if (g >= listed) drawn[a] = -1;  // beyond the list
-                }
-                if (drawn[0] >= 0 && drawn[0] == drawn[1]) {
-                    const u64 x = sh.listed[drawn[0]];
-                    token = index_in(x);
-                    const double of = ends ? (double)kept : 0.5 * (all[0] + all[1]);
-                    logprob = (float)(w.log2_of(key_in(x)) * 0.69314718055994530942 - log(__builtin_ldexp(of, -w.scale)));
-                    done = true;
-                }
-            }
+            if (wave == 0) read_list(sh, par, u, w, f.count, rest, f.whole);
+            __syncthreads();
+            done = uniform((uint32_t)sh.drawn) != 0;
+            token = sh.bin;
+            logprob = sh.logprob;
         }
     }
     if (!done) {

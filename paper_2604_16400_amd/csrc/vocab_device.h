@@ -121,25 +121,21 @@ template <int THREADS> __device__ __forceinline__ double block_sum(double v, dou
     return block_reduce<double, THREADS>(v, s, [](double a, double b) { return a + b; });
 }
 
-// 2^t for t <= 0 as p 2^n with the rounded-off fraction in a polynomial: the Taylor series of e^x at x = f ln 2, |f| <= 1/2,
-// to the power 12 (next term 2.4e-16); 0 for t below -1000
+// 2^t 2^scale as p 2^n, n the nearest integer to t; p(f) = 1 + f q(f) on |f| <= 1/2 with q of degree 7, its coefficients fitted to
+// (2^f - 1) / f by least squares with weights raised until the relative error was the same at all its peaks: 8.2e-13.  0 for t below -1000.
 __device__ __forceinline__ double exp2_neg(double t, int scale)
 {
     const double n = __builtin_rint(t);
-    const double x = (t - n) * 0.69314718055994530942;
-    double p = 1.0 / 479001600.0;
-    p = __builtin_fma(p, x, 1.0 / 39916800.0);
-    p = __builtin_fma(p, x, 1.0 / 3628800.0);
-    p = __builtin_fma(p, x, 1.0 / 362880.0);
-    p = __builtin_fma(p, x, 1.0 / 40320.0);
-    p = __builtin_fma(p, x, 1.0 / 5040.0);
-    p = __builtin_fma(p, x, 1.0 / 720.0);
-    p = __builtin_fma(p, x, 1.0 / 120.0);
-    p = __builtin_fma(p, x, 1.0 / 24.0);
-    p = __builtin_fma(p, x, 1.0 / 6.0);
-    p = __builtin_fma(p, x, 0.5);
-    p = __builtin_fma(p, x, 1.0);
-    p = __builtin_fma(p, x, 1.0);
+    const double f = t - n;
+    double p = 1.3178929944324011e-06;
+    p = __builtin_fma(p, f, 1.5309156437291593e-05);
+    p = __builtin_fma(p, f, 0.00015403825481710473);
+    p = __builtin_fma(p, f, 0.0013333454859321126);
+    p = __builtin_fma(p, f, 0.00961812861609056);
+    p = __builtin_fma(p, f, 0.05550410935267852);
+    p = __builtin_fma(p, f, 0.24022650698110812);
+    p = __builtin_fma(p, f, 0.6931471805482116);
+    p = __builtin_fma(p, f, 1.0);
     return t < -1000.0 ? 0.0 : __builtin_ldexp(p, (int)n + scale);
 }
 
