@@ -513,7 +513,7 @@ int collm_sample(int device, const collm_logits *shape, const void *logits, cons
  * The k largest logits of each row in the order above, and log sum_v exp(z_v / temperature).
  *   values       dev fp32 [n_rows, k];  indices: dev int32 [n_rows, k].  Where a row has fewer than k logits above -inf:
  *                -inf and index -1 behind them.  NaN counts as -inf here.
- *   lse          dev fp32 [n_rows] or NULL; over all logits of the row (a NaN among them: NaN)
+ *   lse          dev fp32 [n_rows] or NULL; over all logits of the row (a NaN among them: NaN; otherwise with +inf: +inf)
  * 1 <= k <= COLLM_MAX_TOP; temperature > 0 and finite.
  */
 int collm_top_logits(int device, const collm_logits *shape, const void *logits, int32_t k, float temperature, float *values, int32_t *indices,
@@ -531,7 +531,8 @@ int collm_top_logits(int device, const collm_logits *shape, const void *logits, 
  *   kd_weight tau (P q_v - p_v - [v outside] r q_v / sum_{outside} q) + ce_weight (softmax(z)_v - [v = label]).
  * An entry of the record whose index is outside [0, vocab) or whose value is -inf is none; a row without any has no KD; p_k = 0
  * adds nothing; where no logit outside the record is above -inf there is no term of r.  A label outside [0, vocab)
- * (say -100) is none.  A row whose logits are all -inf has loss 0 and gradient 0.  NaN logits give NaN.
+ * (say -100) is none.  A row whose logits are all -inf has loss 0 and gradient 0.  NaN and +inf among the logits give
+ * NaN.
  *   values       dev fp32 [n_rows, k];  indices: dev int32 [n_rows, k] (a place named twice counts as often);
  *   lse          dev fp32 [n_rows] or NULL;  labels: dev int32 [n_rows] or NULL
  *   loss         dev fp32 [n_rows]

@@ -382,6 +382,13 @@ __device__ __forceinline__ Weight weight_of(float m, float T, int vocab)
     return w;
 }
 
+// The least logit, in 64 bits, whose weight min-p keeps (-inf where all weights are alike: infinite temperature, also at min_p 1, where
+// the product is no number)
+__device__ __forceinline__ double min_p_logit(const Weight &w, const Params &par)
+{
+    return fmax(w.m + (double)par.T * log((double)par.min_p), (double)kNegInf);
+}
+
 // Puts the list in order (below)
 template <int THREADS> __device__ __forceinline__ bool sort_list(Shared<THREADS> &sh, int count);
 
@@ -409,7 +416,7 @@ __device__ __forceinline__ void sample_by_steps(Shared<THREADS> &sh, const Row<B
     // min-p: the least key whose weight it keeps, and the sum of the weights it keeps
     uint32_t key_min = 0;
     if (par.min_p > 0.0f && !w.top_inf) {
-        const double low = w.m + (double)par.T * log((double)par.min_p);
+        const double low = min_p_logit(w, par);
         const float f = (float)low;
         key_min = key_of(f) + ((double)f < low ? 1 : 0);
     }
@@ -718,7 +725,7 @@ __device__ __forceinline__ bool sample_by_slots(Shared<THREADS> &sh, const Row<t
     }
     // weights, and those that min-p keeps
     double low = kNegInf;
-    if (par.min_p > 0.0f) low = w.m + (double)par.T * log((double)par.min_p);
+    if (par.min_p > 0.0f) low = min_p_logit(w, par);
     u64 sum = 0, over = 0, of_zeros = 0;
     u64 *const weight_of_zero = sh.listed + 2 * kFew;
     if (near_zero) {
@@ -859,12 +866,15 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
         for (int e = 0; e < E; ++e) m = fmaxf(m, Row<BF16>::value(v, e));
         return m;
     };
-    // the bound from the threads' largest logits so far
-    auto raise_bound = [&](int r) {
+    // the bound from the threads' largest logits so far; two sets of words in turn, so that the wait between a call's writes and reads also
+    // keeps the next but one call's writes behind those reads
+    int turn = 0;
+    auto raise_bound = [&]() {
         const uint32_t key = rank_in_wave(top, rank);
-        if (lane == 0) sh.low[r & 1][wave] = key > kKeyNone ? value_of(key) : kLow;
+        if (lane == 0) sh.low[turn][wave] = key > kKeyNone ? value_of(key) : kLow;
         __syncthreads();
-        bound = uniform(fmaxf(-wave_max(-sh.low[r & 1][lane & (W - 1)]), kLow));
+        bound = uniform(fmaxf(-wave_max(-sh.low[turn][lane & (W - 1)]), kLow));
+        turn ^= 1;
     };
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -873,7 +883,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
         const float m = wave_max(top);
         if (lane == 0) sh.top[wave] = m;
     }
-    raise_bound(0);
+    raise_bound();
     {
         // (what the sum is relative to: the largest of the first round)
         const float m = uniform(wave_max(sh.top[lane & (W - 1)]));
@@ -881,7 +891,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     }
     int r = 0;
     for (int c = threadIdx.x; r * kRound < row.whole; ++r, c += kRound) {
-        if (r > 1) raise_bound(r);  // (of the second round nothing is known yet)
+        if (r > 1) raise_bound();  // (of the second round nothing is known yet)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = c + u * THREADS;
@@ -908,7 +918,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
         const float m = wave_max(top);
         if (lane == 0) sh.all[wave] = m;
     }
-    if (r > 1) raise_bound(r);
+    if (r > 1) raise_bound();
     else __syncthreads();
     const float largest_logit = uniform(wave_max(sh.all[lane & (W - 1)]));
     // everything from the last bound on is listed
@@ -937,7 +947,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     f.top = largest_logit;
     f.rest = rest * exp2_neg(-by_T.drift(), 0);
     f.ok = f.count <= kList && queued <= kQueue;
-    f.summed = rest < 1e30 && fabs(by_T.drift() - 32.0) < 1.0;
+    f.summed = rest < 1e30 && fabs(by_T.drift() - 32.0) < 1.0 && f.top < __builtin_huge_valf();
     return f;
 }
 
@@ -1060,7 +1070,7 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
     // the first entries that the cuts leave out
     int cut[2] = {n_k, n_k}, cut_m = n_k;
     if (par.top_p < 1.0f || par.min_p > 0.0f) {
-        const double low = w.m + (double)par.T * log((double)par.min_p);
+        const double low = min_p_logit(w, par);
         u64 before = first;
 #pragma nounroll
         for (int e = begin; e < end; ++e) {
@@ -1203,20 +1213,24 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
             sum += exp2_neg(((double)value_in(sh.listed[e]) - (double)f.ref) * c, 0);
     }
     if (p.lse && !(sorted && f.summed)) {
-        // (relative to each thread's largest logit; of the logits as they are: a NaN among them shows)
+        // (relative to each thread's largest logit; of the logits as they are: a NaN among them shows, also beside +inf)
         Running run;
         const float c = (float)(1.44269504088896340736 / (double)p.temperature), edge[1] = {row.edge(threadIdx.x)};
+        bool nan = edge[0] != edge[0];
         run.add(edge, c);
         for (int k = threadIdx.x; k < row.whole; k += THREADS) {
             const uint4 v = row.body[k];
             float z[Row<BF16>::E];
 #pragma unroll
-            for (int e = 0; e < Row<BF16>::E; ++e) z[e] = Row<BF16>::value(v, e);
+            for (int e = 0; e < Row<BF16>::E; ++e) {
+                z[e] = Row<BF16>::value(v, e);
+                nan |= z[e] != z[e];
+            }
             run.add(z, c);
         }
         f.ref = block_max<THREADS>(run.m, sh.red);
         run.raise(f.ref, c);
-        sum = (double)run.s;
+        sum = f.ref < __builtin_huge_valf() ? (double)run.s : nan ? __builtin_nan("") : __builtin_huge_val();
         f.rest = 0.0;
     }
     if (p.lse) {

@@ -1,0 +1,60 @@
+"""Vocabulary operators at values where formulas lose their meaning, against what the definitions say there."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+
+from oracle import vocab as ov
+from paper_2604_16400_amd import binding as b
+
+pytestmark = pytest.mark.gpu
+INF, NAN = math.inf, math.nan
+
+
+def _torch():
+    import torch
+
+    return torch
+
+
+def _up(x, dtype=None):
+    torch = _torch()
+    return torch.tensor(np.asarray(x), dtype=dtype or torch.float32, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("V,k", [(1, 1), (7, 3), (5000, 64), (50257, 20), (50257, 300)])
+def test_log_sum_exp_beside_infinities(V, k, dtype):
+    """+inf anywhere in the row (among the first logits that are read, the last ones, all): +inf, but NaN where there is a NaN."""
+    torch = _torch()
+    rng = np.random.default_rng(V + k)
+    z = rng.normal(size=(7, V)).astype(np.float32)
+    z[0, 0], z[1, V - 1], z[2], z[3, V // 2] = INF, INF, INF, INF
+    z[3, 0], z[4, V - 1], z[5] = NAN, NAN, -INF
+    values, at, lse = torch.zeros((7, k), device="cuda"), torch.zeros((7, k), dtype=torch.int32, device="cuda"), torch.zeros(7, device="cuda")
+    b.collm_top_logits(_up(z, getattr(torch, dtype)), values, at, lse, temperature=2.0)
+    got = lse.cpu().numpy()
+    assert np.array_equal(got[:3], [INF] * 3) and np.isnan(got[4]) and got[5] == -INF and np.isfinite(got[6])
+    assert np.isnan(got[3])
+    assert at[2].cpu().tolist() == [v if v < V else -1 for v in range(k)]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("V", [5, 3000, 40001])
+def test_sample_at_infinite_temperature(V, dtype):
+    """All weights are alike, so min-p keeps all of them, at 1 too."""
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    par = [(0, 1.0, 0.0), (0, 1.0, 0.5), (0, 1.0, 1.0), (0, 1.0, 2.0), (3, 1.0, 1.0), (300, 0.5, 1.0), (0, 0.25, 1.0)]
+    z = _up(rng.normal(size=(len(par), V)).astype(np.float32), getattr(torch, dtype))
+    u = rng.random(len(par)).astype(np.float32)
+    k, p, m = zip(*par)
+    token, logprob = torch.zeros(len(par), dtype=torch.int32, device="cuda"), torch.zeros(len(par), device="cuda")
+    b.collm_sample(z, _up(u), token, logprob, temperature=_up([INF] * len(par)), top_k=_up(k, torch.int32), top_p=_up(p), min_p=_up(m))
+    host = z.float().cpu().numpy()
+    for i in range(len(par)):
+        want, want_lp = ov.sample(host[i], u[i], INF, k[i], p[i], m[i])
+        assert int(token[i]) == want, (par[i], u[i], int(token[i]), want)
+        assert abs(float(logprob[i]) - want_lp) <= 2.0**-24 * abs(want_lp) + 1e-9
