@@ -183,6 +183,8 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
         entry = lambda f: ctypes.cast(f, ctypes.c_void_p).value
         marshal.bind(torch.bfloat16, torch.float32, PointerTable, entry(lib.collm_lora_linear_fwd), entry(lib.collm_lora_linear_bwd),
                      entry(lib.collm_adapter_adamw), entry(lib.collm_adapter_fedavg))
+        marshal.bind_vocab(torch.int32, entry(lib.collm_sample), entry(lib.collm_top_logits), entry(lib.collm_distill_fwd),
+                           entry(lib.collm_distill_bwd), entry(lib.collm_distill_fwd_bwd))
         _marshal = marshal
     _lib = lib
     return lib
@@ -652,8 +654,29 @@ def _logits(logits, n_rows, rows):
                         _data(rows, (n_rows,), torch.int32, logits, "rows"))
 
 
-def _workspace(workspace):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+def _workspace(workspace, like):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous() or workspace.device != like.device:
+        raise ValueError(f"workspace must be a contiguous tensor on {like.device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _launch(entry, logits, *args):
+    # (behind everything else that an argument may be refused for)
+    if not logits.is_cuda:
+        raise ValueError("logits must be on a GPU")
+    _check(entry(logits.device.index or 0, *args), entry.__name__)
+
+
+def _marshalled(name, logits, rows, workspace, stream, *args):
+    """The call by the compiled marshalling; False where that leaves it to the general path."""
+    if _marshal is None or not logits.is_cuda:
+        return False
+    rc = getattr(_marshal, name)(logits, rows, workspace, _stream_number(stream), *args)
+    if rc:
+        _check(rc, "collm_" + name)
+    return rc is not None
 
 
 def collm_sample(logits, u, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None, rows=None, workspace=None, stream=None):
@@ -662,14 +685,15 @@ def collm_sample(logits, u, token, logprob=None, temperature=None, top_k=None, t
     import torch
 
     lib = load_library()
+    if _marshalled("sample", logits, rows, workspace, stream, u, token, logprob, temperature, top_k, top_p, min_p):
+        return token
     n = int(u.shape[0])
     sh = _logits(logits, n, rows)
     f32 = lambda t, what: _data(t, (n,), torch.float32, logits, what)
     pr = collm_sampling(f32(temperature, "temperature"), _data(top_k, (n,), torch.int32, logits, "top_k"), f32(top_p, "top_p"),
                         f32(min_p, "min_p"))
-    _check(lib.collm_sample(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), f32(u, "u"), ctypes.byref(pr),
-                            _data(token, (n,), torch.int32, logits, "token"), f32(logprob, "logprob"), *_workspace(workspace),
-                            _stream_handle(stream)), "collm_sample")
+    _launch(lib.collm_sample, logits, ctypes.byref(sh), logits.data_ptr(), f32(u, "u"), ctypes.byref(pr),
+            _data(token, (n,), torch.int32, logits, "token"), f32(logprob, "logprob"), *_workspace(workspace, logits), _stream_handle(stream))
     return token
 
 
@@ -679,12 +703,13 @@ def collm_top_logits(logits, values, indices, lse=None, temperature=1.0, rows=No
     import torch
 
     lib = load_library()
+    if _marshalled("top_logits", logits, rows, workspace, stream, values, indices, lse, temperature):
+        return values, indices
     n, k = (int(v) for v in values.shape)
     sh = _logits(logits, n, rows)
-    _check(lib.collm_top_logits(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), k, float(temperature),
-                                _data(values, (n, k), torch.float32, logits, "values"),
-                                _data(indices, (n, k), torch.int32, logits, "indices"), _data(lse, (n,), torch.float32, logits, "lse"),
-                                *_workspace(workspace), _stream_handle(stream)), "collm_top_logits")
+    _launch(lib.collm_top_logits, logits, ctypes.byref(sh), logits.data_ptr(), k, float(temperature),
+            _data(values, (n, k), torch.float32, logits, "values"), _data(indices, (n, k), torch.int32, logits, "indices"),
+            _data(lse, (n,), torch.float32, logits, "lse"), *_workspace(workspace, logits), _stream_handle(stream))
     return values, indices
 
 
@@ -711,12 +736,13 @@ def collm_distill_fwd(logits, t_values, t_indices, loss, stats=None, t_lse=None,
     import torch
 
     lib = load_library()
+    if _marshalled("distill_fwd", logits, rows, workspace, stream, t_values, t_indices, t_lse, labels, temperature, kd_weight,
+                   ce_weight, loss, stats):
+        return loss
     n, d = _teacher(logits, t_values, t_indices, t_lse, labels, temperature, kd_weight, ce_weight)
     sh = _logits(logits, n, rows)
-    _check(lib.collm_distill_fwd(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d),
-                                 _data(loss, (n,), torch.float32, logits, "loss"),
-                                 _data(stats, (n, DISTILL_STATS), torch.float32, logits, "stats"), *_workspace(workspace),
-                                 _stream_handle(stream)), "collm_distill_fwd")
+    _launch(lib.collm_distill_fwd, logits, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d), _data(loss, (n,), torch.float32, logits, "loss"),
+            _data(stats, (n, DISTILL_STATS), torch.float32, logits, "stats"), *_workspace(workspace, logits), _stream_handle(stream))
     return loss
 
 
@@ -727,12 +753,14 @@ def collm_distill_bwd(logits, t_values, t_indices, stats, dloss, dlogits, t_lse=
     import torch
 
     lib = load_library()
+    if _marshalled("distill_bwd", logits, rows, workspace, stream, t_values, t_indices, t_lse, labels, temperature, kd_weight,
+                   ce_weight, stats, dloss, dlogits):
+        return dlogits
     n, d = _teacher(logits, t_values, t_indices, t_lse, labels, temperature, kd_weight, ce_weight)
     sh = _logits(logits, n, rows)
-    _check(lib.collm_distill_bwd(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d),
-                                 _data(stats, (n, DISTILL_STATS), torch.float32, logits, "stats"),
-                                 _data(dloss, (n,), torch.float32, logits, "dloss"), *_grad(logits, dlogits), _stream_handle(stream)),
-           "collm_distill_bwd")
+    _launch(lib.collm_distill_bwd, logits, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d),
+            _data(stats, (n, DISTILL_STATS), torch.float32, logits, "stats"), _data(dloss, (n,), torch.float32, logits, "dloss"),
+            *_grad(logits, dlogits), _stream_handle(stream))
     return dlogits
 
 
@@ -742,9 +770,12 @@ def collm_distill_fwd_bwd(logits, t_values, t_indices, dloss, loss, dlogits, t_l
     import torch
 
     lib = load_library()
+    if _marshalled("distill_fwd_bwd", logits, rows, workspace, stream, t_values, t_indices, t_lse, labels, temperature, kd_weight,
+                   ce_weight, dloss, loss, dlogits):
+        return loss
     n, d = _teacher(logits, t_values, t_indices, t_lse, labels, temperature, kd_weight, ce_weight)
     sh = _logits(logits, n, rows)
-    _check(lib.collm_distill_fwd_bwd(logits.device.index or 0, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d),
-                                     _data(dloss, (n,), torch.float32, logits, "dloss"), _data(loss, (n,), torch.float32, logits, "loss"),
-                                     *_grad(logits, dlogits), *_workspace(workspace), _stream_handle(stream)), "collm_distill_fwd_bwd")
+    _launch(lib.collm_distill_fwd_bwd, logits, ctypes.byref(sh), logits.data_ptr(), ctypes.byref(d),
+            _data(dloss, (n,), torch.float32, logits, "dloss"), _data(loss, (n,), torch.float32, logits, "loss"), *_grad(logits, dlogits),
+            *_workspace(workspace, logits), _stream_handle(stream))
     return loss

@@ -21,7 +21,13 @@ decltype(&collm_lora_linear_fwd) g_linear_fwd = nullptr;
 decltype(&collm_lora_linear_bwd) g_linear_bwd = nullptr;
 decltype(&collm_adapter_adamw) g_adamw = nullptr;
 decltype(&collm_adapter_fedavg) g_fedavg = nullptr;
-PyObject *s_data_ptr, *s_dtype, *s_shape, *s_array, *s_numel, *s_device, *s_index;
+PyObject *g_i32 = nullptr;  // torch.int32; NULL until the entry points below are bound
+decltype(&collm_sample) g_sample = nullptr;
+decltype(&collm_top_logits) g_top_logits = nullptr;
+decltype(&collm_distill_fwd) g_distill_fwd = nullptr;
+decltype(&collm_distill_bwd) g_distill_bwd = nullptr;
+decltype(&collm_distill_fwd_bwd) g_distill_fwd_bwd = nullptr;
+PyObject *s_data_ptr, *s_dtype, *s_shape, *s_array, *s_numel, *s_device, *s_index, *s_stride, *s_is_contiguous, *s_get_device, *s_nbytes;
 
 // Arguments of one call as they are read; `ok` falls at the first one that is not of the expected form.
 struct Reader {
@@ -122,6 +128,60 @@ struct Reader {
         Py_XDECREF(i);
         Py_XDECREF(d);
         return v;
+    }
+    // ---- what the calls on rows of logits take: device tensors, everything about them checked ----
+    int64_t method(PyObject *o, PyObject *name)  // a method without arguments that gives a whole number or a truth value
+    {
+        PyObject *v = ok ? PyObject_CallMethodNoArgs(o, name) : nullptr;
+        const int64_t n = v ? integer(v) : 0;
+        if (!v) ok = false;
+        Py_XDECREF(v);
+        return n;
+    }
+    // [rows, cols] on a GPU, neighbouring columns side by side: address, sizes, elements from row to row, device
+    void *matrix(PyObject *o, int32_t &rows, int32_t &cols, int64_t &ld, int32_t &dev)
+    {
+        shape2(o, rows, cols);
+        PyObject *s = ok ? PyObject_CallMethodNoArgs(o, s_stride) : nullptr;
+        if (s && PyTuple_Check(s) && PyTuple_GET_SIZE(s) == 2) {
+            ld = integer(PyTuple_GET_ITEM(s, 0));
+            if (integer(PyTuple_GET_ITEM(s, 1)) != 1 && cols > 1) ok = false;
+            if (rows <= 1 && ld < cols) ld = cols;
+        } else {
+            ok = false;
+        }
+        Py_XDECREF(s);
+        dev = (int32_t)method(o, s_get_device);
+        if (dev < 0) ok = false;
+        return tensor(o);
+    }
+    // a contiguous tensor of that type on that device, [n] or (cols >= 0) [n, cols]; n < 0: whatever it is; None is NULL if `optional`
+    template <typename T = float> T *data(PyObject *o, PyObject *type, int32_t dev, int32_t &n, int32_t cols = -1, bool optional = false)
+    {
+        if (!ok || (o == Py_None && optional)) return nullptr;
+        PyObject *d = PyObject_GetAttr(o, s_dtype), *s = PyObject_GetAttr(o, s_shape);
+        if (!d || !s || d != type || !PyTuple_Check(s) || PyTuple_GET_SIZE(s) != (cols < 0 ? 1 : 2)) {
+            ok = false;
+        } else {
+            const int32_t rows = int32(PyTuple_GET_ITEM(s, 0));
+            if (n < 0) n = rows;
+            if (rows != n || (cols >= 0 && int32(PyTuple_GET_ITEM(s, 1)) != cols)) ok = false;
+        }
+        Py_XDECREF(d);
+        Py_XDECREF(s);
+        if (!method(o, s_is_contiguous) || method(o, s_get_device) != dev) ok = false;
+        return (T *)tensor(o);
+    }
+    // workspace: address and bytes
+    void *bytes(PyObject *o, int32_t dev, int64_t &size)
+    {
+        size = 0;
+        if (!ok || o == Py_None) return nullptr;
+        PyObject *v = PyObject_GetAttr(o, s_nbytes);
+        size = v ? integer(v) : 0;
+        if (!v || !method(o, s_is_contiguous) || method(o, s_get_device) != dev) ok = false;
+        Py_XDECREF(v);
+        return tensor(o);
     }
     // a contiguous one-dimensional array of elements `fmt` ('i': 32-bit, 'B': bytes) and its length
     const void *array(PyObject *o, char fmt, int32_t &n)
@@ -276,6 +336,145 @@ PyObject *adapter_fedavg(PyObject *, PyObject *const *args, Py_ssize_t n)
     return status(rc);
 }
 
+// The rows of a call: logits, rows, workspace, stream (arguments 0 to 3 of each of the calls below)
+struct Rows {
+    collm_logits sh;
+    void *logits, *workspace, *stream;
+    int64_t workspace_bytes;
+    int32_t dev, n;
+    Reader &r;
+
+    // like: the argument that says how many rows (fp32 [n], or [n, cols] with the number of columns wanted)
+    Rows(Reader &reader, PyObject *like, int32_t *cols) : n(-1), r(reader)
+    {
+        PyObject *const *a = r.args;
+        if (!g_i32) r.ok = false;
+        logits = r.matrix(a[0], sh.n_held, sh.vocab, sh.ld, dev);
+        sh.dtype = r.dtype(a[0]);
+        if (cols) r.shape2(like, n, *cols);
+        else (void)r.data(like, g_f32, dev, n);
+        sh.n_rows = n;
+        sh.rows = r.data<int32_t>(a[1], g_i32, dev, n, -1, true);
+        workspace = r.bytes(a[2], dev, workspace_bytes);
+        stream = r.pointer(a[3]);
+    }
+    float *f32(PyObject *o, int32_t cols = -1) { return r.data(o, g_f32, dev, n, cols, true); }
+    int32_t *i32(PyObject *o, int32_t cols = -1) { return r.data<int32_t>(o, g_i32, dev, n, cols, true); }
+    // a gradient of the logits' shape and type
+    void *grad(PyObject *o, int64_t &ld)
+    {
+        int32_t held = 0, vocab = 0, at = 0;
+        void *p = r.matrix(o, held, vocab, ld, at);
+        if (r.dtype(o) != (collm_dtype)sh.dtype || held != sh.n_held || vocab != sh.vocab || at != dev) r.ok = false;
+        return p;
+    }
+};
+
+#define COLLM_CALL(expr)        \
+    if (!r.ok) Py_RETURN_NONE;  \
+    int rc;                     \
+    Py_BEGIN_ALLOW_THREADS      \
+    rc = (expr);                \
+    Py_END_ALLOW_THREADS        \
+    return status(rc)
+
+// ..., u, token, logprob, temperature, top_k, top_p, min_p
+PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    COLLM_ARGS(11);
+    Rows l(r, args[4], nullptr);
+    const float *u = l.f32(args[4]);
+    int32_t *token = l.i32(args[5]);
+    float *logprob = l.f32(args[6]);
+    collm_sampling p;
+    p.temperature = l.f32(args[7]);
+    p.top_k = l.i32(args[8]);
+    p.top_p = l.f32(args[9]);
+    p.min_p = l.f32(args[10]);
+    COLLM_CALL(g_sample(l.dev, &l.sh, l.logits, u, &p, token, logprob, l.workspace, l.workspace_bytes, l.stream));
+}
+
+// ..., values, indices, lse, temperature
+PyObject *top_logits(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    COLLM_ARGS(8);
+    int32_t k = 0;
+    Rows l(r, args[4], &k);
+    float *values = l.f32(args[4], k);
+    int32_t *indices = l.i32(args[5], k);
+    float *lse = l.f32(args[6]);
+    const float temperature = (float)r.real(args[7]);
+    COLLM_CALL(g_top_logits(l.dev, &l.sh, l.logits, k, temperature, values, indices, lse, l.workspace, l.workspace_bytes, l.stream));
+}
+
+// ..., t_values, t_indices, t_lse, labels, temperature, kd_weight, ce_weight (arguments 4 to 10)
+struct Teacher : Rows {
+    collm_distill d;
+    explicit Teacher(Reader &r) : Rows(r, r.args[4], &d.k)
+    {
+        PyObject *const *a = r.args;
+        d.values = f32(a[4], d.k);
+        d.indices = i32(a[5], d.k);
+        d.lse = f32(a[6]);
+        d.labels = i32(a[7]);
+        d.temperature = (float)r.real(a[8]);
+        d.kd_weight = (float)r.real(a[9]);
+        d.ce_weight = (float)r.real(a[10]);
+    }
+};
+
+// ..., loss, stats
+PyObject *distill_fwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    COLLM_ARGS(13);
+    Teacher t(r);
+    float *loss = t.f32(args[11]), *stats = t.f32(args[12], COLLM_DISTILL_STATS);
+    COLLM_CALL(g_distill_fwd(t.dev, &t.sh, t.logits, &t.d, loss, stats, t.workspace, t.workspace_bytes, t.stream));
+}
+
+// ..., stats, dloss, dlogits
+PyObject *distill_bwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    COLLM_ARGS(14);
+    Teacher t(r);
+    const float *stats = t.f32(args[11], COLLM_DISTILL_STATS), *dloss = t.f32(args[12]);
+    int64_t ld = 0;
+    void *grad = t.grad(args[13], ld);
+    COLLM_CALL(g_distill_bwd(t.dev, &t.sh, t.logits, &t.d, stats, dloss, grad, ld, t.stream));
+}
+
+// ..., dloss, loss, dlogits
+PyObject *distill_fwd_bwd(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    COLLM_ARGS(14);
+    Teacher t(r);
+    const float *dloss = t.f32(args[11]);
+    float *loss = t.f32(args[12]);
+    int64_t ld = 0;
+    void *grad = t.grad(args[13], ld);
+    COLLM_CALL(g_distill_fwd_bwd(t.dev, &t.sh, t.logits, &t.d, dloss, loss, grad, ld, t.workspace, t.workspace_bytes, t.stream));
+}
+
+// torch.int32 and the addresses of the five entry points on rows of logits
+PyObject *bind_vocab(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    COLLM_ARGS(6);
+    void *f[5];
+    for (int i = 0; i < 5; ++i) {
+        f[i] = r.pointer(args[1 + i]);
+        if (!f[i]) r.ok = false;
+    }
+    if (!r.ok) Py_RETURN_FALSE;
+    g_sample = reinterpret_cast<decltype(g_sample)>(f[0]);
+    g_top_logits = reinterpret_cast<decltype(g_top_logits)>(f[1]);
+    g_distill_fwd = reinterpret_cast<decltype(g_distill_fwd)>(f[2]);
+    g_distill_bwd = reinterpret_cast<decltype(g_distill_bwd)>(f[3]);
+    g_distill_fwd_bwd = reinterpret_cast<decltype(g_distill_fwd_bwd)>(f[4]);
+    Py_INCREF(args[0]);
+    Py_XSETREF(g_i32, args[0]);
+    Py_RETURN_TRUE;
+}
+
 // the two element types as torch has them, the class of pointer tables, and the addresses of the four entry points
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -298,7 +497,9 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 
 #define COLLM_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {COLLM_METHOD(linear_fwd),     COLLM_METHOD(linear_bwd), COLLM_METHOD(adapter_adamw),
-                         COLLM_METHOD(adapter_fedavg), COLLM_METHOD(bind), {nullptr, nullptr, 0, nullptr}};
+                         COLLM_METHOD(adapter_fedavg), COLLM_METHOD(bind),       COLLM_METHOD(sample),
+                         COLLM_METHOD(top_logits),     COLLM_METHOD(distill_fwd), COLLM_METHOD(distill_bwd),
+                         COLLM_METHOD(distill_fwd_bwd), COLLM_METHOD(bind_vocab), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -312,5 +513,9 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_numel = PyUnicode_InternFromString("numel");
     s_device = PyUnicode_InternFromString("device");
     s_index = PyUnicode_InternFromString("index");
+    s_stride = PyUnicode_InternFromString("stride");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    s_nbytes = PyUnicode_InternFromString("nbytes");
     return PyModule_Create(&module);
 }

@@ -58,3 +58,46 @@ def test_sample_at_infinite_temperature(V, dtype):
         want, want_lp = ov.sample(host[i], u[i], INF, k[i], p[i], m[i])
         assert int(token[i]) == want, (par[i], u[i], int(token[i]), want)
         assert abs(float(logprob[i]) - want_lp) <= 2.0**-24 * abs(want_lp) + 1e-9
+
+
+def test_both_marshalling_routes_give_the_same_call(monkeypatch):
+    """Compiled marshalling against the general path: the same results of plain arguments, the same refusals of others."""
+    torch = _torch()
+    rng = np.random.default_rng(4)
+    n, held, V, k, ld = 9, 12, 1003, 7, 1040
+    z = torch.zeros((held, ld), dtype=torch.bfloat16, device="cuda")[:, :V]
+    z.copy_(_up(rng.normal(size=(held, V))))
+    rows = _up(rng.permutation(held)[:n], torch.int32)
+    ws = torch.zeros(b.VOCAB_WORKSPACE, dtype=torch.uint8, device="cuda")
+    f = lambda lo=0.0: _up(lo + rng.random(n))
+    u, temp, top_p, min_p, dloss, top_k = f(), f(0.5), f(), f(-0.9), f(), _up(rng.integers(0, 30, n), torch.int32)
+    labels = _up(rng.integers(-1, V, n), torch.int32)
+    new = lambda *shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype, device="cuda")
+
+    def everything():
+        out = [new(n, dtype=torch.int32), new(n), new(n, k), new(n, k, dtype=torch.int32), new(n), new(n), new(n, b.DISTILL_STATS), torch.zeros_like(z),
+               new(n), torch.zeros((held, V + 5), dtype=z.dtype, device="cuda")[:, :V]]
+        token, lp, tv, ti, lse, loss, stats, grad, loss2, grad2 = out
+        kw = dict(rows=rows, workspace=ws)
+        assert b.collm_sample(z, u, token, lp, temp, top_k, top_p, min_p, **kw) is token
+        assert b.collm_top_logits(z, tv, ti, lse, 2.0, **kw)[0] is tv
+        t = dict(t_lse=lse, labels=labels, temperature=2.0, kd_weight=0.25, ce_weight=0.5, **kw)
+        assert b.collm_distill_fwd(z, tv + 0.5, ti, loss, stats, **t) is loss
+        assert b.collm_distill_bwd(z, tv + 0.5, ti, stats, dloss, grad, **t) is grad
+        assert b.collm_distill_fwd_bwd(z, tv + 0.5, ti, dloss, loss2, grad2, **t) is loss2
+        for bad in (dict(u=u.double()), dict(u=u[:4]), dict(token=token.long()), dict(rows=rows[::2]), dict(top_k=temp), dict(temperature=temp.cpu()),
+                    dict(logits=z.half()), dict(logits=z.t()), dict(logits=z.cpu()), dict(workspace=ws.cpu())):
+            with pytest.raises((ValueError, TypeError)):
+                b.collm_sample(**{**dict(logits=z, u=u, token=token, rows=rows), **bad})
+        for bad in (dict(dlogits=grad[:3]), dict(dlogits=grad.float()), dict(t_indices=ti[:, :3]), dict(loss=loss[:2]), dict(labels=labels.long())):
+            with pytest.raises(ValueError):
+                b.collm_distill_fwd_bwd(**{**dict(logits=z, t_values=tv, t_indices=ti, dloss=dloss, loss=loss2, dlogits=grad, rows=rows), **bad})
+        with pytest.raises(RuntimeError):
+            b.collm_top_logits(z, tv, ti, temperature=-1.0, **kw)
+        return out
+
+    assert b._marshal is not None
+    first = everything()
+    monkeypatch.setattr(b, "_marshal", None)
+    for x, y in zip(first, everything()):
+        assert torch.equal(x, y)
