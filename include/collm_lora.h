@@ -471,9 +471,10 @@ int collm_adapter_adamw(int device, collm_dtype dtype, void *param, float *maste
  *                those of a mixed batch), or NULL: rows 0 .. n_rows - 1 (n_rows <= n_held).  An entry outside
  *                [0, n_held) is a row that is not there: token -1, an empty record, loss 0.  Where gradients are
  *                written the entries must differ from each other.
- *   workspace    dev, 16-byte aligned, workspace_bytes long, contents free, or NULL (0 bytes): calls of few rows cut each row into
- *                parts and keep the parts' results there; where it does not suffice (COLLM_VOCAB_WORKSPACE bytes always do)
- *                they take a row at a time, which is slower.  Calls that overlap in time need workspaces of their own.
+ *   workspace    dev, 16-byte aligned, workspace_bytes long, contents free, or NULL (0 bytes): collm_distill_fwd_bwd shares few long rows
+ *                among several blocks each and keeps what those find there (COLLM_VOCAB_WORKSPACE bytes always suffice); without it
+ *                a row is one block's, which is slower.  The other calls take a workspace for the same use and need none so far.
+ *                Calls that overlap in time need workspaces of their own.
  * Limits: 1 <= vocab <= 1048576; COLLM_E_SHAPE otherwise.
  */
 #define COLLM_VOCAB_WORKSPACE (16 << 20)

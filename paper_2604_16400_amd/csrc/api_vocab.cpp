@@ -178,6 +178,8 @@ int collm_distill_fwd_bwd(int device, const collm_logits *shape, const void *log
     a.dloss = dloss;
     a.dlogits = dlogits;
     a.ld_grad = ld_grad;
+    a.workspace = workspace;
+    a.workspace_bytes = workspace_bytes;
     HIP_TRY(hipSetDevice(device));
     HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
     HIP_TRY(launch_distill_fwd_bwd(a, (hipStream_t)stream));

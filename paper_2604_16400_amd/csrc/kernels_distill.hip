@@ -63,10 +63,27 @@ __device__ __forceinline__ Entry load_place(const DistillArgs &p, int i, int j, 
     }
     return e;
 }
-template <bool BF16> __device__ __forceinline__ void load_logit(Entry &e, const Row<BF16> &row)
+template <bool BF16, typename S = void> __device__ __forceinline__ void load_logit(Entry &e, const Row<BF16> &row, const S *span = nullptr)
 {
-    if (e.at < 0 || e.at >= row.n || !(e.t > kNegInf)) e.at = -1;
-    else e.z = Elem<BF16>::load(row.row, e.at);
+    if (e.at < 0 || e.at >= row.n || !(e.t > kNegInf)) {
+        e.at = -1;
+        return;
+    }
+    if constexpr (!std::is_void_v<S>)
+        if (!span->has(row, e.at)) return;  // (another block's, which may have written there already)
+    e.z = Elem<BF16>::load(row.row, e.at);
+}
+template <bool BF16> __device__ __forceinline__ void put_entry(const Record &rec, int j, const Entry &e, const Row<BF16> &row)
+{
+    rec.at[j] = e.at;
+    rec.t[j] = e.t;
+    rec.z[j] = e.z;
+    bool first = false;
+    if (e.at >= 0) {
+        const int b = row.bit(e.at);
+        first = !(atomicOr(&rec.bits[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u);
+    }
+    rec.first[j] = first;
 }
 
 // Row i's record into shared memory, its places into the bitmap.  mine: the entry of this thread's index, loaded before.
@@ -79,15 +96,7 @@ __device__ __forceinline__ void put_record(const Record &rec, const DistillArgs 
             e = load_place(p, i, j, row.n > 0);
             load_logit(e, row);
         }
-        rec.at[j] = e.at;
-        rec.t[j] = e.t;
-        rec.z[j] = e.z;
-        bool first = false;
-        if (e.at >= 0) {
-            const int b = row.bit(e.at);
-            first = !(atomicOr(&rec.bits[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u);
-        }
-        rec.first[j] = first;
+        put_entry(rec, j, e, row);
     }
 }
 template <bool BF16, int THREADS>
@@ -182,6 +191,24 @@ __device__ __forceinline__ Teacher read_record(const Record &rec, const DistillA
     return out;
 }
 
+// A block's share of a row: chunks [begin, end), the first share's with the row's edges
+struct Span {
+    int begin, end;
+    bool edges;
+    __device__ __forceinline__ Span(int part, int parts, int whole) : edges(part == 0)
+    {
+        const int each = (whole + parts - 1) / parts;
+        begin = part * each < whole ? part * each : whole;
+        end = begin + each < whole ? begin + each : whole;
+    }
+    // whether element `at` of the row is of this share
+    template <bool BF16> __device__ __forceinline__ bool has(const Row<BF16> &row, int at) const
+    {
+        const int b = row.bit(at);
+        return b < row.whole * Row<BF16>::E ? b >= begin * Row<BF16>::E && b < end * Row<BF16>::E : edges;
+    }
+};
+
 // What the gradient of a row is made of, for dloss = 1; kept for the backward call as kDistillStats floats.
 //   outside the record  u (one + second u), u = exp((z - ref) / tau), at temperatures 1 and 2 (a label's term is a power of u);
 //                       elsewhere one u + second exp(z - ref)
@@ -197,6 +224,71 @@ struct Coef {
     {
         kd = flags & kHasKd ? uniform(p.kd_weight * p.temperature * g) : 0.f;
         label = flags & kHasLabel ? uniform(p.ce_weight * g) : 0.f;
+    }
+};
+
+// A row's coefficients and loss from its record and the sums over the rest of it.  rest, rest_ce: sums of exp((z - ref) / tau) and exp(z - ref), as
+// they are times 2^drift and 2^drift_ce
+struct Finish {
+    const Teacher &t;
+    float ref, max;
+    double rest, inv, to_rest, to_in, rest_scale, sum, sum_ce, second_scale, mass, r, kd, ce_weight;
+    int label;
+    bool any, live, two;
+    __device__ __forceinline__ Finish(const DistillArgs &p, const Teacher &teacher, float ref_, double rest_, double rest_ce, double drift, double drift_ce,
+                                      int label_, bool tail, bool two_)
+        : t(teacher), ref(ref_), rest(rest_), label(label_), two(two_)
+    {
+        const double log2e = 1.44269504088896340736;
+        any = rest != 0.0;  // (NaN is something)
+        const bool held_some = t.in != 0.0;
+        max = held_some ? (any ? fmaxf(ref, t.ref) : t.ref) : ref;
+        inv = 1.0 / (double)p.temperature;
+        // what turns the sums into sums relative to `max`, as powers of 2
+        to_rest = any ? ((double)ref - (double)max) * inv * log2e - drift : 0.0;
+        const double to_rest_ce = any ? ((double)ref - (double)max) * log2e - drift_ce : 0.0;
+        to_in = held_some ? (double)t.ref - (double)max : 0.0;
+        rest_scale = exp2_neg(to_rest, 0);
+        second_scale = two ? exp2_neg(to_rest_ce, 0) : rest_scale;
+        sum = rest * rest_scale;
+        if (tail) sum += t.in * exp2_neg(to_in * inv * log2e, 0);
+        sum_ce = sum;
+        if (two) {
+            sum_ce = rest_ce * second_scale;
+            if (tail) sum_ce += t.in_ce * exp2_neg(to_in * log2e, 0);
+        }
+        live = sum != 0.0;
+        r = tail && any && t.some ? t.r : 0.0;
+        mass = t.p_sum + r;
+        kd = (double)p.kd_weight * (double)p.temperature;
+        ce_weight = (double)p.ce_weight;
+    }
+    __device__ __forceinline__ void coefficients(float *coef, bool near) const
+    {
+        const double over = 1.0 / sum, ce = live && label >= 0 ? ce_weight / sum_ce : 0.0;
+        double one = live && t.some ? kd * (mass * rest_scale * over - (r > 0.0 ? r / rest : 0.0)) : 0.0;
+        if (!two) one += ce * rest_scale;  // (temperature 1: the same exponentials)
+        coef[0] = any ? ref : 0.f;
+        coef[1] = (float)one;
+        coef[2] = two ? (float)(ce * second_scale) : 0.f;
+        coef[3] = live ? max : 0.f;
+        coef[4] = live && t.some ? (float)(kd * mass * over) : 0.f;
+        coef[5] = (float)ce;
+        coef[6] = __uint_as_float((near ? kNear : 0) | (live && t.some ? kHasKd : 0) | (live && label >= 0 ? kHasLabel : 0));
+        coef[7] = 0.f;
+    }
+    __device__ __forceinline__ double loss(const DistillArgs &p, float label_z) const
+    {
+        double out = 0.0;
+        if (!live) return out;
+        const double log_sum = log(sum);
+        if (t.some) {
+            out = t.entropy - t.cross + t.p_sum * (log_sum - to_in * inv);
+            if (r > 0.0) out += r * (log(r) - (log(rest) + to_rest * 0.69314718055994530942 - log_sum));
+            out *= kd * (double)p.temperature;
+        }
+        if (label >= 0) out += ce_weight * (log(sum_ce) - ((double)label_z - (double)max));
+        return out;
     }
 };
 
@@ -264,33 +356,37 @@ template <bool BF16, bool ONCE> struct Gradient {
         Elem<BF16>::store(grad, row.edge_index(threadIdx.x), g[0]);
     }
     template <int THREADS>
-    __device__ __forceinline__ void corrections(const Record &rec, const DistillArgs &p, const Row<BF16> &row, int label, float label_z,
-                                                bool label_in_record) const
+    __device__ __forceinline__ void corrections(const Record &rec, const DistillArgs &p, const Row<BF16> &row, const Span &span, int label,
+                                                float label_z, bool label_in_record) const
+    {
+        for (int j = threadIdx.x; j < p.k; j += THREADS)
+            if (rec.at[j] >= 0 && rec.first[j] && span.has(row, rec.at[j])) entry(rec.at[j], rec.z[j], rec.p[j], p, label);
+        if (label >= 0 && !label_in_record && threadIdx.x == 0 && span.has(row, label)) at_label(label, label_z);
+    }
+    // at a place of the record: its logit, its probability
+    __device__ __forceinline__ void entry(int at, float z, double prob, const DistillArgs &p, int label) const
     {
         const Exp kd(p.temperature, c.max), ce(1.0f, c.max);
-        for (int j = threadIdx.x; j < p.k; j += THREADS) {
-            const int at = rec.at[j];
-            if (at < 0 || !rec.first[j]) continue;
-            const float z = rec.z[j];
-            double g = (double)(c.in * kd(z)) - (double)c.kd * rec.p[j];
-            if (c.ce != 0.0f) g += (double)(c.ce * ce(z)) - (at == label ? (double)c.label : 0.0);
-            Elem<BF16>::store(grad, at, (float)g);
-        }
-        if (label >= 0 && !label_in_record && threadIdx.x == 0) {
-            float g[8];
-            const float z[1] = {label_z};
-            outside(g, z);
-            Elem<BF16>::store(grad, label, g[0] - c.label);
-        }
+        double g = (double)(c.in * kd(z)) - (double)c.kd * prob;
+        if (c.ce != 0.0f) g += (double)(c.ce * ce(z)) - (at == label ? (double)c.label : 0.0);
+        Elem<BF16>::store(grad, at, (float)g);
+    }
+    // at the label, outside the record
+    __device__ __forceinline__ void at_label(int label, float label_z) const
+    {
+        float g[8];
+        const float z[1] = {label_z};
+        outside(g, z);
+        Elem<BF16>::store(grad, label, g[0] - c.label);
     }
 };
 
-// f(chunk, its number, that it is not held) over a row's chunks from `begin` on, U loads on the way at any time; BACK: the last ones first
-template <bool BF16, int THREADS, int U, bool ONCE, bool BACK, typename F> __device__ __forceinline__ void stream(const Row<BF16> &row, int begin, F f)
+// f(chunk, its number, that it is not held) over a row's chunks [begin, end), U loads on the way at any time; BACK: the last ones first
+template <bool BF16, int THREADS, int U, bool ONCE, bool BACK, typename F> __device__ __forceinline__ void stream(const Row<BF16> &row, int begin, int end, F f)
 {
     const __amdgpu_buffer_rsrc_t from = row.buffer();  // (reads outside the row, before it too, give 0)
     constexpr int kStep = U * THREADS;
-    const int steps = (row.whole - begin + kStep - 1) / kStep;
+    const int steps = (end - begin + kStep - 1) / kStep;
     int c = begin + (int)threadIdx.x + (BACK ? (steps - 1) * kStep : 0);
     uint4 v[U];
 #pragma unroll
@@ -299,7 +395,7 @@ template <bool BF16, int THREADS, int U, bool ONCE, bool BACK, typename F> __dev
         const int next = BACK ? c - kStep : c + kStep;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (c + u * THREADS < row.whole) f(v[u], c + u * THREADS, std::false_type());
+            if (c + u * THREADS < end) f(v[u], c + u * THREADS, std::false_type());
             v[u] = load_chunk<ONCE>(from, next + u * THREADS);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -325,7 +421,7 @@ template <bool BF16, int THREADS, int SLOTS, bool ONCE> struct Held {
             then(s, t);
             __builtin_amdgcn_sched_barrier(0);
         }
-        stream<BF16, THREADS, SLOTS ? 1 : 4, SLOTS == 0 && ONCE, false>(row, SLOTS * THREADS, f);  // (beside what is held it is read again)
+        stream<BF16, THREADS, SLOTS ? 1 : 4, SLOTS == 0 && ONCE, false>(row, SLOTS * THREADS, row.whole, f);  // (beside what is held it is read again)
     }
     template <typename F> __device__ __forceinline__ void each(const Row<BF16> &row, F f)
     {
@@ -491,52 +587,11 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ vo
         }
         take_record_off<BF16, THREADS>(rec, p, row);
         if (wave == 0) {
-            const bool any = rest != 0.0;  // (NaN is something)
-            const bool held_some = t.in != 0.0;
-            const float max = held_some ? (any ? fmaxf(ref, t.ref) : t.ref) : ref;
-            const double inv = 1.0 / (double)p.temperature, log2e = 1.44269504088896340736;
-            // what turns the sums into sums relative to `max`, as powers of 2
-            const double to_rest = any ? ((double)ref - (double)max) * inv * log2e - drift : 0.0;
-            const double to_rest_ce = any ? ((double)ref - (double)max) * log2e - drift_ce : 0.0;
-            const double to_in = held_some ? (double)t.ref - (double)max : 0.0;
-            const double rest_scale = exp2_neg(to_rest, 0), rest_scale_ce = two ? exp2_neg(to_rest_ce, 0) : rest_scale;
-            double sum = rest * rest_scale;
-            if (tail) sum += t.in * exp2_neg(to_in * inv * log2e, 0);
-            double sum_ce = sum;
-            if (two) {
-                sum_ce = rest_ce * rest_scale_ce;
-                if (tail) sum_ce += t.in_ce * exp2_neg(to_in * log2e, 0);
-            }
-            const bool live = sum != 0.0;
-            const double r = tail && any && t.some ? t.r : 0.0, mass = t.p_sum + r, kd = (double)p.kd_weight * (double)p.temperature;
-            const double over = 1.0 / sum;
-            const double ce = live && label >= 0 ? (double)p.ce_weight / sum_ce : 0.0;
-            double one = live && t.some ? kd * (mass * rest_scale * over - (r > 0.0 ? r / rest : 0.0)) : 0.0;
-            double second = 0.0;
-            if (two) second = ce * rest_scale_ce;
-            else one += ce * rest_scale;  // (temperature 1: the same exponentials)
-            if (lane == 0) {
-                sh.coef[0] = any ? ref : 0.f;
-                sh.coef[1] = (float)one;
-                sh.coef[2] = (float)second;
-                sh.coef[3] = live ? max : 0.f;
-                sh.coef[4] = live && t.some ? (float)(kd * mass * over) : 0.f;
-                sh.coef[5] = (float)ce;
-                sh.coef[6] = __uint_as_float((near ? kNear : 0) | (live && t.some ? kHasKd : 0) | (live && label >= 0 ? kHasLabel : 0));
-                sh.coef[7] = 0.f;
-            }
+            const Finish end(p, t, ref, rest, rest_ce, drift, drift_ce, label, tail, two);
+            if (lane == 0) end.coefficients(sh.coef, near);
             if (GRAD) __syncthreads();
             // (the loss itself while the other waves go on)
-            double loss = 0.0;
-            if (live) {
-                const double log_sum = log(sum);
-                if (t.some) {
-                    loss = t.entropy - t.cross + t.p_sum * (log_sum - to_in * inv);
-                    if (r > 0.0) loss += r * (log(r) - (log(rest) + to_rest * 0.69314718055994530942 - log_sum));
-                    loss *= kd * (double)p.temperature;
-                }
-                if (label >= 0) loss += (double)p.ce_weight * (log(sum_ce) - ((double)label_z - (double)max));
-            }
+            const double loss = end.loss(p, label_z);
             if (lane == 0) p.loss[i] = (float)loss;
             if (p.stats && lane < kDistillStats) p.stats[(int64_t)i * kDistillStats + lane] = sh.coef[lane];
         } else if (GRAD) {
@@ -548,7 +603,7 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ vo
             held.each(row, [&](uint4 &v, int k, auto) { g.chunk(row, v, k); }, [&](int s, int t) { held.load(from, s, t); });
             g.edges(row, edge_z);
             __syncthreads();
-            g.template corrections<THREADS>(rec, p, row, label, label_z, label_in_record);
+            g.template corrections<THREADS>(rec, p, row, Span(0, 1, row.whole), label, label_z, label_in_record);
         } else {
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s) held.load(from, s, threadIdx.x);
@@ -561,43 +616,227 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ vo
 }
 
 // The gradient from what the forward call kept.  Rows and their chunks go from the last to the first: the forward call left the last-read
-// ones in the last-level cache.
-template <bool BF16, int THREADS, bool ONCE> __global__ void __launch_bounds__(THREADS, 8) distill_bwd_kernel(DistillArgs p)
+// ones in the last-level cache.  A row is `parts` blocks', each reading of the logits what it writes the gradient of (which may lie in their
+// place); the record's probabilities are worked out by each.
+template <bool BF16, int THREADS, bool ONCE> __global__ void __launch_bounds__(THREADS, 8) distill_bwd_kernel(DistillArgs p, int parts)
 {
     extern __shared__ double mem[];
     const Record rec(mem, p.k, p.r.vocab);
     uint32_t *const bits = rec.bits;
-    const int i = p.r.n_rows - 1 - (int)blockIdx.x;
+    const int block = (int)blockIdx.x / parts, i = p.r.n_rows - 1 - block;
     const void *at = row_of(p.r, i);
     if (!at) return;
     const Row<BF16> row(at, p.r.vocab);
+    const Span span((int)blockIdx.x - block * parts, parts, row.whole);
     for (int w = threadIdx.x; w < (row.n + 31) / 32; w += THREADS) bits[w] = 0;
     __syncthreads();
-    Entry mine = load_place(p, i, threadIdx.x, true);
-    load_logit(mine, row);
-    put_record<BF16, THREADS>(rec, p, i, row, mine);
+    for (int j = threadIdx.x; j < p.k; j += THREADS) {
+        Entry e = load_place(p, i, j, true);
+        load_logit(e, row, &span);
+        put_entry(rec, j, e, row);
+    }
     int label = p.labels ? p.labels[i] : -1;
     if (label >= row.n) label = -1;
-    const float label_z = label >= 0 ? Elem<BF16>::load(at, label) : 0.f, edge_z = row.edge(threadIdx.x);
+    const float label_z = label >= 0 && span.has(row, label) ? Elem<BF16>::load(at, label) : 0.f, edge_z = row.edge(threadIdx.x);
     __syncthreads();  // (every thread has read what it needs beside its chunks: the gradient may lie in the place of the logits)
     const int b = label >= 0 ? row.bit(label) : 0;
     const bool label_in_record = label >= 0 && (bits[b >> 5] >> (b & 31) & 1u);
     if (threadIdx.x < kWave) read_record(rec, p, i, kNegInf, false, false);
     const Gradient<BF16, ONCE> g(Coef(p.stats + (int64_t)i * kDistillStats, p, p.dloss[i]), p, row, p.r.rows ? (int64_t)p.r.rows[i] : i);
-    stream<BF16, THREADS, 4, false, true>(row, 0, [&](const uint4 &v, int k, auto) { g.chunk(row, v, k); });
-    g.edges(row, edge_z);
+    stream<BF16, THREADS, 4, false, true>(row, span.begin, span.end, [&](const uint4 &v, int k, auto) { g.chunk(row, v, k); });
+    if (span.edges) g.edges(row, edge_z);
     __syncthreads();
-    g.template corrections<THREADS>(rec, p, row, label, label_z, label_in_record);
+    g.template corrections<THREADS>(rec, p, row, span, label, label_z, label_in_record);
 }
 
-template <int THREADS, typename K> hipError_t launch(K kernel, int blocks, const DistillArgs &a, hipStream_t st)
+// ---- few rows: loss and gradient by many blocks a row, in two launches ----
+// What the first launch leaves of a row in the workspace: the record's part by a block of its own, the sums over the rest by `parts` blocks, each
+// relative to the largest logit it met.
+struct Head {
+    Teacher t;
+    int label;
+    float label_z;
+    bool label_in_record;
+};
+struct Part {
+    double s, ce;
+    float m;
+};
+struct Kept {
+    Head *head;
+    Part *parts;
+    double *p;
+    float *z;
+    int32_t *at;  // -1: no entry, or not its place's first
+    static __host__ __device__ int64_t bytes(int k, int parts) { return ((int64_t)sizeof(Head) + parts * (int64_t)sizeof(Part) + k * (int64_t)16 + 15) / 16 * 16; }
+    __device__ __forceinline__ Kept(const DistillArgs &a, int i, int n_parts)
+        : head((Head *)((char *)a.workspace + i * bytes(a.k, n_parts))), parts((Part *)(head + 1)), p((double *)(parts + n_parts)), z((float *)(p + a.k)),
+          at((int32_t *)(z + a.k))
+    {
+    }
+};
+static_assert(sizeof(Head) % 8 == 0 && sizeof(Part) % 8 == 0, "what follows them is 8-byte aligned");
+
+// Block (row, part), the row's last block its record's
+template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS) distill_parts_kernel(DistillArgs p, int parts)
+{
+    constexpr int E = Row<BF16>::E, U = 4, W = THREADS / kWave;
+    extern __shared__ double mem[];
+    __shared__ Shared<THREADS> sh;
+    const int i = (int)blockIdx.x / (parts + 1), part = (int)blockIdx.x - i * (parts + 1);
+    const int lane = threadIdx.x & (kWave - 1), wave = (int)uniform((uint32_t)threadIdx.x / kWave);
+    const void *start = row_of(p.r, i);
+    if (!start) return;
+    const Row<BF16> row(start, p.r.vocab);
+    const Kept kept(p, i, parts);
+    const bool tail = p.t_lse != nullptr;
+    int label = (int)uniform((uint32_t)(p.labels ? p.labels[i] : -1));
+    if (label < 0 || label >= row.n) label = -1;
+    const bool two = label >= 0 && p.temperature != 1.0f;
+    if (part == parts) {
+        const Record rec(mem, p.k, p.r.vocab);
+        Entry mine = load_place(p, i, threadIdx.x, true);
+        for (int w = threadIdx.x; w < (row.n + 31) / 32; w += THREADS) rec.bits[w] = 0;
+        load_logit(mine, row);
+        const float label_z = label >= 0 ? Elem<BF16>::load(start, label) : 0.f;
+        __syncthreads();
+        put_record<BF16, THREADS>(rec, p, i, row, mine);
+        __syncthreads();
+        const float z_max = largest_in_record(rec, p.k);
+        if (wave == 0) {
+            const Teacher t = read_record(rec, p, i, z_max, true, two);
+            if (lane == 0) {
+                const int b = label >= 0 ? row.bit(label) : 0;
+                kept.head->t = t;
+                kept.head->label = label;
+                kept.head->label_z = label_z;
+                kept.head->label_in_record = label >= 0 && (rec.bits[b >> 5] >> (b & 31) & 1u);
+            }
+        }
+        __syncthreads();
+        for (int j = threadIdx.x; j < p.k; j += THREADS) {
+            kept.p[j] = rec.p[j];
+            kept.z[j] = rec.z[j];
+            kept.at[j] = rec.first[j] ? rec.at[j] : -1;
+        }
+        return;
+    }
+    // this part of the rest of the row; the bitmap is of its chunks and, behind them, of the edges
+    const Span span(part, parts, row.whole);
+    uint32_t *const bits = (uint32_t *)mem;
+    const __amdgpu_buffer_rsrc_t from = row.buffer();
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_chunk<false>(from, span.begin + u * THREADS + (int)threadIdx.x);
+    const int first = span.begin * E, here = (span.end - span.begin) * E;
+    float edge_z = span.edges ? row.edge(threadIdx.x) : kNegInf;
+    if (tail) {
+        for (int w = threadIdx.x; w < (here + 2 * E + 31) / 32; w += THREADS) bits[w] = 0;
+        __syncthreads();
+        for (int j = threadIdx.x; j < p.k; j += THREADS) {
+            const Entry e = load_place(p, i, j, true);
+            if (e.at < 0 || e.at >= row.n || !(e.t > kNegInf) || !span.has(row, e.at)) continue;
+            const int b = row.bit(e.at), to = b < row.whole * E ? b - first : here + (b - row.whole * E);
+            atomicOr(&bits[to >> 5], 1u << (to & 31));
+        }
+        __syncthreads();
+        const int e = here + (int)threadIdx.x;
+        if (span.edges && (int)threadIdx.x < row.edges && (bits[e >> 5] >> (e & 31) & 1u)) edge_z = kNegInf;
+    }
+    const float c = (float)(1.44269504088896340736 / (double)p.temperature);
+    Running run;
+    {
+        const float z[1] = {edge_z};
+        run.add(z, c);
+    }
+    for (int k = span.begin + (int)threadIdx.x; k < span.end; k += U * THREADS) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = k + u * THREADS;
+            if (at < span.end) {
+                if (tail) mask_chunk<BF16>(v[u], bits, at - span.begin);
+                float z[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) z[e] = Row<BF16>::value(v[u], e);
+                run.add(z, c);
+            }
+            v[u] = load_chunk<false>(from, at + U * THREADS);
+        }
+    }
+    const float m = wave_max(run.m);
+    run.raise(m, c);
+    const double s = wave_sum((double)run.s), ce = wave_sum((double)run.ce);
+    if (lane == 0) {
+        sh.max[wave] = m;
+        sh.sum[wave] = s;
+        sh.sum_ce[wave] = ce;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        const float wave_m = lane < W ? sh.max[lane] : kLow, top = wave_max(wave_m);
+        const double all = wave_sum(lane < W ? sh.sum[lane] * (double)__builtin_amdgcn_exp2f((wave_m - top) * c) : 0.0);
+        const double all_ce = wave_sum(lane < W ? sh.sum_ce[lane] * (double)__builtin_amdgcn_exp2f((wave_m - top) * 1.44269504f) : 0.0);
+        if (lane == 0) kept.parts[part] = {all, all_ce, top};
+    }
+}
+
+// Block (row, part): every wave joins the sums; the gradient of the part, the loss by the first part's last wave.  Of the logits only the part's
+// own are read, as the gradient may lie in their place.
+template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS) distill_join_kernel(DistillArgs p, int parts)
+{
+    const int i = (int)blockIdx.x / parts, part = (int)blockIdx.x - i * parts;
+    const int lane = threadIdx.x & (kWave - 1);
+    const void *start = row_of(p.r, i);
+    if (!start) {
+        if (part == 0 && threadIdx.x == 0) p.loss[i] = 0.0f;
+        return;
+    }
+    const Row<BF16> row(start, p.r.vocab);
+    const Span span(part, parts, row.whole);
+    const Kept kept(p, i, parts);
+    const float edge_z = row.edge(threadIdx.x);
+    const Teacher t = kept.head->t;
+    const int label = kept.head->label;
+    const float label_z = kept.head->label_z, c = (float)(1.44269504088896340736 / (double)p.temperature);
+    const Part mine = lane < parts ? kept.parts[lane] : Part{0.0, 0.0, kLow};
+    const float ref = uniform(wave_max(mine.m));
+    const double rest = uniform(wave_sum(mine.s * (double)__builtin_amdgcn_exp2f((mine.m - ref) * c)));
+    const double rest_ce = uniform(wave_sum(mine.ce * (double)__builtin_amdgcn_exp2f((mine.m - ref) * 1.44269504f)));
+    const bool two = label >= 0 && p.temperature != 1.0f;
+    const Finish end(p, t, ref, rest, rest_ce, 0.0, 0.0, label, p.t_lse != nullptr, two);
+    float coef[kDistillStats];
+    end.coefficients(coef, false);
+    const Gradient<BF16, false> g(Coef(coef, p, p.dloss[i]), p, row, p.r.rows ? (int64_t)__builtin_amdgcn_readfirstlane(p.r.rows[i]) : i);
+    stream<BF16, THREADS, 4, false, false>(row, span.begin, span.end, [&](const uint4 &v, int k, auto) { g.chunk(row, v, k); });
+    if (span.edges) g.edges(row, edge_z);
+    __syncthreads();
+    for (int j = threadIdx.x; j < p.k; j += THREADS) {
+        const int at = kept.at[j];
+        if (at >= 0 && span.has(row, at)) g.entry(at, kept.z[j], kept.p[j], p, label);
+    }
+    if (threadIdx.x == 0 && label >= 0 && !kept.head->label_in_record && span.has(row, label)) g.at_label(label, label_z);
+    if (part == 0 && threadIdx.x == THREADS - 1) p.loss[i] = (float)end.loss(p, label_z);
+}
+
+// Shares of a row that together with those of the other rows make up to `blocks` blocks, none below 1024 chunks; rows of up to 4096, which one block
+// reads in four loads a thread, are not shared.  (A share of 512 chunks takes no less time, and with twice the blocks every one waits for its record.)
+constexpr int kMostParts = kWave;
+int parts_of(const DistillArgs &a, int chunks, int blocks)
+{
+    if (chunks <= 4 * 1024) return 1;
+    int parts = blocks / a.r.n_rows;
+    if (parts > chunks / 1024) parts = chunks / 1024;
+    return parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts;
+}
+
+template <int THREADS, typename K, typename... More> hipError_t launch(K kernel, int blocks, const DistillArgs &a, hipStream_t st, More... more)
 {
     const size_t bytes = Record::bytes(a.k, a.r.vocab);  // up to 150 KiB
     if (bytes + sizeof(Shared<THREADS>) > (64u << 10)) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return e;
     }
-    COLLM_LAUNCH(kernel, dim3(blocks), dim3(THREADS), bytes, st, a);
+    COLLM_LAUNCH(kernel, dim3(blocks), dim3(THREADS), bytes, st, a, more...);
     return hipGetLastError();
 }
 
@@ -621,7 +860,15 @@ template <bool BF16, bool ONCE> hipError_t launch_many(const DistillArgs &a, int
 }
 template <bool BF16> hipError_t launch_step(const DistillArgs &a, hipStream_t st)
 {
-    const int chunks = a.r.vocab / Row<BF16>::E;
+    const int chunks = a.r.vocab / Row<BF16>::E, parts = parts_of(a, chunks, a.compute_units);
+    // Shares of a quarter of a row or less: one / 32 / 64 rows of 128256 bf16 22.6 / 24.4 / 25.8 -> 11.2 / 15.5 / 20.8 us, one row of 160000 fp32
+    // 33.8 -> 11.1 (bf16 64000: 14.5 -> 11.8).  Halves lose: the logits are read twice, in two launches (128 rows of 128256: 29.4 -> 31.3).
+    if (parts >= 4 && a.workspace_bytes >= a.r.n_rows * Kept::bytes(a.k, parts)) {
+        const hipError_t e = launch<512>(distill_parts_kernel<BF16, 512>, a.r.n_rows * (parts + 1), a, st, parts);
+        if (e != hipSuccess) return e;
+        COLLM_LAUNCH((distill_join_kernel<BF16, 512>), dim3(a.r.n_rows * parts), dim3(512), 0, st, a, parts);
+        return hipGetLastError();
+    }
     if (past_the_cache(a.r)) return launch_many<BF16, true>(a, chunks, st);
     if (a.r.n_rows <= a.compute_units) {
         if (chunks <= 1024 * 4) return launch_held<BF16, 1024, 4, false>(a, st);
@@ -641,9 +888,12 @@ template <bool BF16, bool ONCE> hipError_t launch_loss(const DistillArgs &a, hip
 
 template <bool BF16, bool ONCE> hipError_t launch_gradient(const DistillArgs &a, hipStream_t st)
 {
-    if (a.r.n_rows >= 4 * a.compute_units) return launch<256>(distill_bwd_kernel<BF16, 256, ONCE>, a.r.n_rows, a, st);
-    if (a.r.n_rows >= 2 * a.compute_units) return launch<512>(distill_bwd_kernel<BF16, 512, ONCE>, a.r.n_rows, a, st);
-    return launch<1024>(distill_bwd_kernel<BF16, 1024, ONCE>, a.r.n_rows, a, st);
+    if (a.r.n_rows >= 4 * a.compute_units) return launch<256>(distill_bwd_kernel<BF16, 256, ONCE>, a.r.n_rows, a, st, 1);
+    if (a.r.n_rows >= 2 * a.compute_units) return launch<512>(distill_bwd_kernel<BF16, 512, ONCE>, a.r.n_rows, a, st, 1);
+    // (a block for every second compute unit: forward and backward of one / 64 rows of 128256 bf16 21.4 / 25.1 -> 16.7 / 22.0 us, one row of
+    // 160000 fp32 27.8 -> 19; with a block for each 32 rows take 20.2 instead of 19.3)
+    const int parts = parts_of(a, a.r.vocab / Row<BF16>::E, a.compute_units / 2);
+    return launch<1024>(distill_bwd_kernel<BF16, 1024, ONCE>, a.r.n_rows * parts, a, st, parts);
 }
 
 }  // namespace

@@ -53,6 +53,8 @@ struct DistillArgs {
     void *dlogits;
     int64_t ld_grad;
     int compute_units;        // of the GPU
+    void *workspace;          // of the call that does both
+    int64_t workspace_bytes;
 };
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t st);
