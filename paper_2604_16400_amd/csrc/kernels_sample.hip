@@ -68,11 +68,13 @@ struct Weight {
     int scale;    // a weight of 1 is 2^scale
     bool top_inf;
     __device__ __forceinline__ double log2_of(uint32_t key) const { return ((double)value_of(key) - m) * c; }
-    __device__ __forceinline__ u64 operator()(uint32_t key) const
+    __device__ __forceinline__ u64 operator()(uint32_t key) const { return of(value_of(key)); }
+    // (of a logit above -inf)
+    __device__ __forceinline__ u64 of(float z) const
     {
-        if (top_inf) return value_of(key) == __builtin_huge_valf() ? (u64)1 << scale : 0;
+        if (top_inf) return z == __builtin_huge_valf() ? (u64)1 << scale : 0;
         // (added to 2^52, the last bit of the sum's fraction is worth 1: the rounding of that sum is the rounding)
-        const double w = exp2_neg(log2_of(key), scale) + 4503599627370496.0;
+        const double w = exp2_neg(((double)z - m) * c, scale) + 4503599627370496.0;
         return (u64)__double_as_longlong(w) & (((u64)1 << 52) - 1);
     }
 };
@@ -183,8 +185,13 @@ template <bool BF16, int THREADS> struct Steps {
 
     __device__ __forceinline__ Steps(Shared<THREADS> &s, const Row<BF16> &r) : sh(s), row(r) {}
 
-    // f(key, index) over the row's logits, four loads on the way at any time
+    // f(key, index) over the row's logits
     template <typename F> __device__ __forceinline__ void each(F f) const
+    {
+        each_value([&](float z, int idx) { f(key_of(z), idx); });
+    }
+    // f(logit, index) over the row's logits, four loads on the way at any time
+    template <typename F> __device__ __forceinline__ void each_value(F f) const
     {
         constexpr int E = Row<BF16>::E, U = 4;
         const __amdgpu_buffer_rsrc_t from = row.buffer();
@@ -197,12 +204,12 @@ template <bool BF16, int THREADS> struct Steps {
                 const int at = c + u * THREADS;
                 if (at < row.whole) {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) f(key_of(Row<BF16>::value(v[u], e)), row.lo + at * E + e);
+                    for (int e = 0; e < E; ++e) f(Row<BF16>::value(v[u], e), row.lo + at * E + e);
                 }
                 v[u] = load_chunk<false>(from, at + U * THREADS);
             }
         }
-        if ((int)threadIdx.x < row.edges) f(key_of(row.edge(threadIdx.x)), row.edge_index(threadIdx.x));
+        if ((int)threadIdx.x < row.edges) f(row.edge(threadIdx.x), row.edge_index(threadIdx.x));
     }
     __device__ __forceinline__ void clear(u64 *hist) const
     {
@@ -213,10 +220,7 @@ template <bool BF16, int THREADS> struct Steps {
     // (0: nothing).  Returns the total.
     template <typename M> __device__ __forceinline__ u64 first(float m, float lo, M measure)
     {
-        hi = m;
-        scale = fminf((float)(kBins - 1) / (m - lo), 1e30f);
-        if (!(scale >= 0.f)) scale = 0.f;
-        clear(sh.hist[0]);
+        begin(m, lo);
         each([&](uint32_t key, int idx) {
             if (key <= kKeyNone) return;
             const u64 x = measure(key, idx);
@@ -226,9 +230,44 @@ template <bool BF16, int THREADS> struct Steps {
         scan = Scan<THREADS>(sh, sh.hist[0]);
         return scan.total;
     }
-    __device__ __forceinline__ int step(uint32_t key) const
+    __device__ __forceinline__ void begin(float m, float lo)
     {
-        return (int)fminf(fmaxf((hi - value_of(key)) * scale, 0.f), (float)(kBins - 1));
+        hi = m;
+        scale = fminf((float)(kBins - 1) / (m - lo), 1e30f);
+        if (!(scale >= 0.f)) scale = 0.f;
+        clear(sh.hist[0]);
+    }
+    // The same of the weights of all logits; over: the sum of those of logits from `low` on that this thread met
+    __device__ __forceinline__ u64 first_of_weights(float m, float lo, const Weight &w, float low, u64 &over)
+    {
+        begin(m, lo);
+        each_value([&](float z, int) {
+            if (!(z > kNegInf)) return;
+            const u64 x = w.of(z);
+            if (z >= low) over += x;
+            if (x) atomicAdd(&sh.hist[0][step_of(z)], x);
+        });
+        __syncthreads();
+        scan = Scan<THREADS>(sh, sh.hist[0]);
+        return scan.total;
+    }
+    __device__ __forceinline__ int step_of(float z) const { return (int)fminf(fmaxf((hi - z) * scale, 0.f), (float)(kBins - 1)); }
+    __device__ __forceinline__ int step(uint32_t key) const { return step_of(value_of(key)); }
+    // Bounds outside which no logit is of the steps from `from` to `to`: (hi - z) scale is rounded twice in step_of, by 2^-24 each
+    __device__ __forceinline__ void bounds(int from, int to, float &least, float &most) const
+    {
+        least = kNegInf;
+        most = __builtin_huge_valf();
+        if (to < kBins - 1 && scale > 0.f) {
+            const double z = (double)hi - (double)(to + 1) / (double)scale * (1.0 + 0x1p-20);
+            least = (float)z;
+            if ((double)least > z) least = nextafterf(least, kNegInf);
+        }
+        if (from > 0) {
+            const double z = (double)hi - (double)from / (double)scale * (1.0 - 0x1p-20);
+            most = (float)z;
+            if ((double)most < z) most = nextafterf(most, __builtin_huge_valf());
+        }
     }
     // The spot at which what `measure` counts, as in the first histogram, reaches `goal` (1 <= goal <= total)
     template <typename M> __device__ __forceinline__ Spot find(u64 goal, M measure) const
@@ -422,11 +461,17 @@ __device__ __forceinline__ void sample_by_steps(Shared<THREADS> &sh, const Row<B
     }
     u64 over = 0;
     const float end = fmaxf(least, m - 44.0f * par.T);
-    const u64 total = steps.first(m, end, [&](uint32_t key, int idx) {
-        const u64 x = inside(key, idx);
-        if (key >= key_min) over += x;
-        return x;
-    });
+    const bool all = last == ~(u64)0;
+    u64 total;
+    if (all) {
+        total = steps.first_of_weights(m, end, w, key_min > kKeyNone ? value_of(key_min) : kNegInf, over);
+    } else {
+        total = steps.first(m, end, [&](uint32_t key, int idx) {
+            const u64 x = inside(key, idx);
+            if (key >= key_min) over += x;
+            return x;
+        });
+    }
     if (key_min) over = block_reduce<u64, THREADS>(over, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
     else over = total;
     const double p_goal = ceil((double)par.top_p * (double)total);
@@ -453,8 +498,13 @@ __device__ __forceinline__ void sample_by_steps(Shared<THREADS> &sh, const Row<B
     const u64 above_1 = draw_above[0];
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
-    steps.each([&](uint32_t key, int idx) {
-        if (key <= kKeyNone) return;
+    // (most logits are told from their value alone)
+    float draw_least, draw_most, cut_least = __builtin_huge_valf(), cut_most = kNegInf;
+    steps.bounds(bin_1, bin_2, draw_least, draw_most);
+    if (cut_bin >= 0) steps.bounds(cut_bin, cut_bin, cut_least, cut_most);
+    steps.each_value([&](float z, int idx) {
+        if (!((z >= draw_least && z <= draw_most) || (z >= cut_least && z <= cut_most)) || !(z > kNegInf)) return;
+        const uint32_t key = key_of(z);
         const int b = steps.step(key);
         if (((b < bin_1 || b > bin_2) && b != cut_bin) || entry(key, idx) > last) return;
         const int to = atomicAdd(&sh.count, 1);
