@@ -729,79 +729,74 @@ __device__ __forceinline__ bool sample_by_slots(Shared<THREADS> &sh, const Row<t
     const int near_zero = (int)uniform((uint32_t)sh.count);
     if (uniform((uint32_t)sh.queued) || near_zero > kFew) return false;
     if (near_zero) Steps<true, THREADS>(sh, row).sort_few(near_zero);
-    // thread t has slots N t .. N t + N - 1 in the order of the row; the logits near 0 are in front of thread kMiddle's
-    auto slot_at = [&](int o) { return o < kHalf ? kHalf - 1 - o : o; };
+    // Thread t has slots N t .. N t + N - 1 in the order of the row; the logits near 0 are in front of thread kMiddle's.  What occurs is put side by
+    // side, in order: entries of a key and how often.  Few slots are in use, and those are neighbours: so every thread gets its share.
     auto key_at = [&](int o) { return key_of(bf16_to_f32(o < kHalf ? kNearest + (kHalf - 1 - o) : 0x8000u + kNearest + (o - kHalf))); };
-    int first = kSlots, own = 0;
-#pragma unroll
-    for (int n = N - 1; n >= 0; --n) {
-        const int o = threadIdx.x * N + n, times = (int)sh.times[slot_at(o)];
-        if (times) first = o;
-        own += times;
-    }
-    first = (int)-block_max<THREADS>((float)-first, sh.red);  // of the largest logit, but for those near 0
     const u64 *zeros = sh.listed + kFew;
-    if (first == kSlots && !near_zero) return false;
-    const float m = near_zero && first >= kHalf ? value_in(zeros[0]) : value_of(key_at(first));
-    const Weight w = weight_of(m, par.T, row.n);
-    int zeros_kept = near_zero;
-    // how many the top-k keeps of each slot
-    if (par.k) {
-        int incl = own;
+    u64 *const entries = sh.binned;  // (in the place of the counters)
+    uint32_t count_of[N];
+    u64 both = 0;  // entries << 32 | logits
 #pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const int up = __shfl_up(incl, o);
-            if (lane >= o) incl += up;
-        }
-        if (lane == kWave - 1) sh.wave_sum[wave] = (u64)incl;
-        __syncthreads();
-        int run = incl - own, all = near_zero;
-        for (int k = 0; k < W; ++k) {
-            if (k < wave) run += (int)sh.wave_sum[k];
-            all += (int)sh.wave_sum[k];
-        }
-        if (threadIdx.x == kMiddle) sh.cut_m = run >= par.k ? 0 : par.k - run < near_zero ? par.k - run : near_zero;
-        __syncthreads();
-        zeros_kept = (int)uniform((uint32_t)sh.cut_m);
-        if (all < par.k) return false;  // (what is beyond the slots may be asked for)
-        if (threadIdx.x >= kMiddle) run += near_zero;
+    for (int n = 0; n < N; ++n) {
+        const int o = threadIdx.x * N + n;
+        count_of[n] = sh.times[o < kHalf ? kHalf - 1 - o : o];
+        both += count_of[n] ? (u64)1 << 32 | count_of[n] : 0;
+    }
+    u64 up_to = both;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const u64 up = __shfl_up(up_to, o);
+        if (lane >= o) up_to += up;
+    }
+    if (lane == kWave - 1) sh.wave_sum[wave] = up_to;
+    __syncthreads();  // (every counter has been read)
+    u64 in_all = 0, before_zeros = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        if (k == wave) up_to += in_all;
+        if (k == kMiddle / kWave) before_zeros = in_all;
+        in_all += sh.wave_sum[k];
+    }
+    const int n_entries = (int)uniform((uint32_t)(in_all >> 32)) + near_zero, zeros_at = (int)uniform((uint32_t)(before_zeros >> 32));
+    const int n_logits = (int)uniform((uint32_t)in_all) + near_zero, zeros_run = (int)uniform((uint32_t)before_zeros);
+    // (what is beyond the slots may be asked for; more different logits than a list holds)
+    if (n_entries == 0 || n_entries > kList || (par.k && n_logits < par.k)) return false;
+    {
+        const bool behind = (int)threadIdx.x >= kMiddle;
+        int at = (int)((up_to - both) >> 32) + (behind ? near_zero : 0), run = (int)(uint32_t)(up_to - both) + (behind ? near_zero : 0);
+        // (how many the top-k keeps)
+        auto kept_of = [&](int times, int before) { return !par.k || before + times <= par.k ? times : before < par.k ? par.k - before : 0; };
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            uint32_t &times = sh.times[slot_at(threadIdx.x * N + n)];
-            const int left = par.k - run;
-            run += (int)times;
-            if (left < (int)times) times = left > 0 ? (uint32_t)left : 0;
+            if (!count_of[n]) continue;
+            entries[at++] = (u64)key_at(threadIdx.x * N + n) << 32 | (uint32_t)kept_of((int)count_of[n], run);
+            run += (int)count_of[n];
         }
+        if ((int)threadIdx.x < near_zero)
+            entries[zeros_at + threadIdx.x] = (u64)key_in(zeros[threadIdx.x]) << 32 | (uint32_t)kept_of(1, zeros_run + (int)threadIdx.x);
     }
-    // weights, and those that min-p keeps
-    double low = kNegInf;
-    if (par.min_p > 0.0f) low = min_p_logit(w, par);
-    u64 sum = 0, over = 0, of_zeros = 0;
-    u64 *const weight_of_zero = sh.listed + 2 * kFew;
-    if (near_zero) {
-        u64 x = 0;
-        if ((int)threadIdx.x < zeros_kept) {
-            x = w(key_in(zeros[threadIdx.x]));
-            if ((double)value_in(zeros[threadIdx.x]) >= low) over = x;
-            weight_of_zero[threadIdx.x] = x;
+    __syncthreads();
+    const float m = value_of((uint32_t)(entries[0] >> 32));
+    const Weight w = weight_of(m, par.T, row.n);
+    // weights, a thread those of `each` entries, and those that min-p keeps
+    constexpr int kEach = kList / THREADS;
+    const int each = (n_entries + THREADS - 1) / THREADS;
+    const double low = par.min_p > 0.0f ? min_p_logit(w, par) : kNegInf;
+    u64 one[kEach], sum = 0, over = 0;
+    uint32_t times[kEach];
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+        const int e = threadIdx.x * each + n;
+        times[n] = 0;
+        one[n] = 0;
+        if (n < each && e < n_entries) {
+            const uint32_t key = (uint32_t)(entries[e] >> 32);
+            times[n] = (uint32_t)entries[e];
+            one[n] = w(key);
+            if ((double)value_of(key) >= low) over += one[n] * times[n];
         }
-        of_zeros = block_reduce<u64, THREADS>(x, sh.wave_sum, [](u64 a, u64 b) { return a + b; });
+        sum += one[n] * times[n];
     }
-    // f(weight of the slots so far, of one logit of this slot, how many, its place in the order) over the thread's slots that occur
-    auto each_slot = [&](u64 run, auto f) {
-#pragma nounroll
-        for (int o = threadIdx.x * N; o < (int)threadIdx.x * N + N; ++o) {
-            const uint32_t times = sh.times[slot_at(o)];
-            if (!times) continue;
-            const u64 one = w(key_at(o));
-            f(run, one, times, o);
-            run += one * times;
-        }
-        return run;
-    };
-    sum = each_slot(0, [&](u64, u64 one, uint32_t times, int o) {
-        if ((double)value_of(key_at(o)) >= low) over += one * times;
-    });
     u64 incl = sum;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
@@ -817,27 +812,22 @@ __device__ __forceinline__ bool sample_by_slots(Shared<THREADS> &sh, const Row<t
         total += sh.wave_sum[k];
     }
     __syncthreads();
-    total += of_zeros;
-    if (threadIdx.x >= kMiddle) incl += of_zeros;
     const u64 begin = incl - sum;
-    // where the running sum reaches `goal`: the slot (kSlots: near 0), how many of it (from 1), and the sum with those
+    // where the running sum reaches `goal`: the entry, how many of it (from 1), and the sum with those
     auto find = [&](u64 goal, int &slot, uint32_t &q, u64 &with) {
         if (goal > begin && goal <= incl) {
-            each_slot(begin, [&](u64 run, u64 one, uint32_t times, int o) {
-                if (goal <= run || goal > run + one * times) return;
-                const uint32_t many = (uint32_t)((goal - run + one - 1) / one);
-                sh.bin = o;
-                sh.drawn = (int)many;
-                sh.above = run + many * one;
-            });
-        }
-        if (threadIdx.x == kMiddle && goal <= begin && goal > begin - of_zeros) {
-            u64 x = begin - of_zeros;
-            int many = 0;
-            while (x < goal) x += weight_of_zero[many++];
-            sh.bin = kSlots;
-            sh.drawn = many;
-            sh.above = x;
+            u64 run = begin;
+#pragma unroll
+            for (int n = 0; n < kEach; ++n) {
+                const u64 all = one[n] * times[n];
+                if (goal > run && goal <= run + all) {
+                    const uint32_t many = (uint32_t)((goal - run + one[n] - 1) / one[n]);
+                    sh.bin = threadIdx.x * each + n;
+                    sh.drawn = (int)many;
+                    sh.above = run + many * one[n];
+                }
+                run += all;
+            }
         }
         __syncthreads();
         slot = (int)uniform((uint32_t)sh.bin);
@@ -859,12 +849,11 @@ __device__ __forceinline__ bool sample_by_slots(Shared<THREADS> &sh, const Row<t
     }
     const double goal = floor((double)u * (double)kept);
     find(!(goal >= 0.0) ? 1 : goal >= (double)(kept - 1) ? kept : (u64)goal + 1, slot, q, with);
-    uint32_t key;
-    if (slot == kSlots) {
-        key = key_in(zeros[q - 1]);
-        token = index_in(zeros[q - 1]);
+    const uint32_t key = uniform((uint32_t)(entries[slot] >> 32));
+    if (slot >= zeros_at && slot < zeros_at + near_zero) {
+        token = index_in(zeros[slot - zeros_at]);
     } else {
-        key = key_at(slot);
+        __syncthreads();  // (the counters of what follows take the entries' place)
         token = locate_bits<THREADS>(sh, row, __float_as_uint(value_of(key)) >> 16, q);
     }
     logprob = (float)(w.log2_of(key) * 0.69314718055994530942 - log(__builtin_ldexp((double)kept, -w.scale)));
