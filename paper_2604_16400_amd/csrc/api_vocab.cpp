@@ -103,6 +103,7 @@ int collm_sample(int device, const collm_logits *shape, const void *logits, cons
     a.token = token;
     a.logprob = logprob;
     HIP_TRY(hipSetDevice(device));
+    HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
     HIP_TRY(launch_sample(a, (hipStream_t)stream));
     return COLLM_OK;
 }

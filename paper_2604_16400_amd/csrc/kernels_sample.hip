@@ -587,8 +587,9 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u16x2 halves(uint32_t w) { return __builtin_bit_cast(u16x2, w); }
 
 // The index of the q-th lowest (from 1) of the logits whose bf16 bits are `bits` (not a zero's): counted by runs of 128 chunks,
-// then within the run.
-template <int THREADS> __device__ __forceinline__ int locate_bits(Shared<THREADS> &sh, const Row<true> &row, uint32_t bits, uint32_t q)
+// then within the run.  held: the row's chunks in registers (SLOTS of them a thread; 0: read again).
+template <int THREADS, int SLOTS>
+__device__ __forceinline__ int locate_bits(Shared<THREADS> &sh, const Row<true> &row, const uint4 (&held)[SLOTS ? SLOTS : 1], uint32_t bits, uint32_t q)
 {
     constexpr int U = 4, kRun = 2 * kWave;
     const int lane = threadIdx.x & (kWave - 1), runs = (row.whole + kRun - 1) / kRun;
@@ -613,26 +614,35 @@ template <int THREADS> __device__ __forceinline__ int locate_bits(Shared<THREADS
     const bool at_edge = (int)threadIdx.x < row.edges && ((const uint16_t *)row.row)[row.edge_index(threadIdx.x)] == (uint16_t)bits;
     if (at_edge) atomicAdd(&hist[(int)threadIdx.x < row.lo ? 0 : 1 + runs], (u64)1);
     if (at_edge && (int)threadIdx.x < row.lo) atomicAdd(&sh.count, 1);
-    const __amdgpu_buffer_rsrc_t from = row.buffer();
-    uint4 v[U];
+    if constexpr (SLOTS > 0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load_chunk<false>(from, u * THREADS + threadIdx.x);
-    // (as far as the q-th: half the row, on average)
-    for (int c = threadIdx.x, done = 0; done < row.whole; c += U * THREADS, done += U * THREADS) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = c + u * THREADS;
-            if (at < row.whole && any_in_chunk(v[u])) {
-                const int n = __popc(in_chunk(v[u]));
-                atomicAdd(&hist[1 + at / kRun], (u64)n);
-                atomicAdd(&sh.count, n);
-            }
-            v[u] = load_chunk<false>(from, at + U * THREADS);
+        for (int k = 0; k < SLOTS; ++k) {
+            const int at = k * THREADS + (int)threadIdx.x;
+            if (at < row.whole && any_in_chunk(held[k])) atomicAdd(&hist[1 + at / kRun], (u64)__popc(in_chunk(held[k])));
         }
         __syncthreads();
-        const bool met = uniform((uint32_t)sh.count) >= q;
-        __syncthreads();
-        if (met) break;
+    } else {
+        const __amdgpu_buffer_rsrc_t from = row.buffer();
+        uint4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = load_chunk<false>(from, u * THREADS + threadIdx.x);
+        // (as far as the q-th: half the row, on average)
+        for (int c = threadIdx.x, done = 0; done < row.whole; c += U * THREADS, done += U * THREADS) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = c + u * THREADS;
+                if (at < row.whole && any_in_chunk(v[u])) {
+                    const int n = __popc(in_chunk(v[u]));
+                    atomicAdd(&hist[1 + at / kRun], (u64)n);
+                    atomicAdd(&sh.count, n);
+                }
+                v[u] = load_chunk<false>(from, at + U * THREADS);
+            }
+            __syncthreads();
+            const bool met = uniform((uint32_t)sh.count) >= q;
+            __syncthreads();
+            if (met) break;
+        }
     }
     int bin;
     u64 above;
@@ -669,16 +679,22 @@ template <int THREADS> __device__ __forceinline__ int locate_bits(Shared<THREADS
 // logit from 2^17 on among its logits, or many near 0).
 //   slot t + kSlots / 2 (if negative): magnitude kNearest + t in bf16 bits.  In the order of the row: positive logits, t falling; those nearer to 0 than any
 //   slot, listed; negative ones, t rising
-template <int THREADS>
+template <int THREADS, int SLOTS>
 __device__ __forceinline__ bool sample_by_slots(Shared<THREADS> &sh, const Row<true> &row, const Params &par, float u, int &token, float &logprob)
 {
     constexpr int U = 4, N = kSlots / THREADS, W = THREADS / kWave, kHalf = kSlots / 2, kMiddle = kHalf / N;
     constexpr uint32_t kNearest = 0x3800u;  // 2^-15
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const __amdgpu_buffer_rsrc_t from = row.buffer();
-    uint4 v[U];
+    constexpr int kHeld = SLOTS ? SLOTS : 1, kAhead = SLOTS ? 1 : U;
+    uint4 held[kHeld], v[kAhead];
+    if constexpr (SLOTS > 0) {
 #pragma unroll
-    for (int k = 0; k < U; ++k) v[k] = load_chunk<false>(from, k * THREADS + threadIdx.x);
+        for (int k = 0; k < SLOTS; ++k) held[k] = load_chunk<false>(from, k * THREADS + threadIdx.x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < U; ++k) v[k] = load_chunk<false>(from, k * THREADS + threadIdx.x);
+    }
     for (int k = threadIdx.x; k < kSlots / 4; k += THREADS) ((uint4 *)sh.times)[k] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 0) sh.count = sh.queued = 0;
     __syncthreads();
@@ -695,34 +711,64 @@ __device__ __forceinline__ bool sample_by_slots(Shared<THREADS> &sh, const Row<t
         }
     };
     if ((int)threadIdx.x < row.edges) count(((const uint16_t *)row.row)[row.edge_index(threadIdx.x)], row.edge_index(threadIdx.x));
-    for (int c = threadIdx.x; c < row.whole; c += U * THREADS) {
+    auto count_chunk = [&](const uint4 &c, int at) {
+        if (at >= row.whole) return;
+        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+        // two logits at a time: the bits less kNearest have a slot where bits 12 to 14 are clear
+        u16x2 x[4];
+        uint32_t out = 0;
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int at = c + k * THREADS;
-            if (at < row.whole) {
-                const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-                // two logits at a time: the bits less kNearest have a slot where bits 12 to 14 are clear
-                u16x2 x[4];
-                uint32_t out = 0;
+        for (int j = 0; j < 4; ++j) {
+            x[j] = halves(w[j]) - u16x2{(uint16_t)kNearest, (uint16_t)kNearest};
+            out |= __builtin_bit_cast(uint32_t, x[j]) & 0x70007000u;
+        }
+        if (!out) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[j] = halves(w[j]) - u16x2{(uint16_t)kNearest, (uint16_t)kNearest};
-                    out |= __builtin_bit_cast(uint32_t, x[j]) & 0x70007000u;
-                }
-                if (!out) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const u16x2 sign = x[j] >> u16x2{15, 15};
-                        const uint32_t to = __builtin_bit_cast(uint32_t, (u16x2)((x[j] << u16x2{2, 2}) + sign * u16x2{4 * kHalf, 4 * kHalf}));  // in bytes
-                        atomicAdd((uint32_t *)((char *)sh.times + (to & 0xffffu)), 1u);
-                        atomicAdd((uint32_t *)((char *)sh.times + (to >> 16)), 1u);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) count((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu, row.lo + at * 8 + e);
-                }
+            for (int j = 0; j < 4; ++j) {
+                const u16x2 sign = x[j] >> u16x2{15, 15};
+                const uint32_t to = __builtin_bit_cast(uint32_t, (u16x2)((x[j] << u16x2{2, 2}) + sign * u16x2{4 * kHalf, 4 * kHalf}));  // in bytes
+                atomicAdd((uint32_t *)((char *)sh.times + (to & 0xffffu)), 1u);
+                atomicAdd((uint32_t *)((char *)sh.times + (to >> 16)), 1u);
             }
-            v[k] = load_chunk<false>(from, at + U * THREADS);
+        } else if constexpr (SLOTS > 0) {
+            // (those above -inf: of a masked row, whose chunks all come here, few; in a loop, as this is compiled SLOTS times: unrolled, 256 rows of
+            // 128256 take 42 us instead of 35)
+            uint32_t left = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const u16x2 some = __builtin_elementwise_min((u16x2)(halves(w[j]) ^ u16x2{0xff80, 0xff80}), u16x2{1, 1});
+                const uint32_t two = __builtin_bit_cast(uint32_t, some);
+                left |= ((two | two >> 15) & 3u) << (2 * j);
+            }
+            for (; left; left &= left - 1) {
+                const int e = __ffs(left) - 1;
+                const uint32_t pair = e < 4 ? (e < 2 ? w[0] : w[1]) : (e < 6 ? w[2] : w[3]);
+                count((e & 1) ? pair >> 16 : pair & 0xffffu, row.lo + at * 8 + e);
+            }
+        } else {
+            // (pairs of -inf, as in most of a masked row's chunks, have none; the loop above would take registers that this has not: 1024 rows 102 -> 110 us)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (w[j] == 0xff80ff80u) continue;
+                count(w[j] & 0xffffu, row.lo + at * 8 + 2 * j);
+                count(w[j] >> 16, row.lo + at * 8 + 2 * j + 1);
+            }
+        }
+    };
+    if constexpr (SLOTS > 0) {
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            count_chunk(held[k], k * THREADS + (int)threadIdx.x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+        for (int c = threadIdx.x; c < row.whole; c += U * THREADS) {
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int at = c + k * THREADS;
+                count_chunk(v[k], at);
+                v[k] = load_chunk<false>(from, at + U * THREADS);
+            }
         }
     }
     __syncthreads();
@@ -854,7 +900,7 @@ __device__ __forceinline__ bool sample_by_slots(Shared<THREADS> &sh, const Row<t
         token = index_in(zeros[slot - zeros_at]);
     } else {
         __syncthreads();  // (the counters of what follows take the entries' place)
-        token = locate_bits<THREADS>(sh, row, __float_as_uint(value_of(key)) >> 16, q);
+        token = locate_bits<THREADS, SLOTS>(sh, row, held, __float_as_uint(value_of(key)) >> 16, q);
     }
     logprob = (float)(w.log2_of(key) * 0.69314718055994530942 - log(__builtin_ldexp((double)kept, -w.scale)));
     return true;
@@ -1173,7 +1219,7 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
 }
 
 // One block a row.  What bounds it: one pass over the row, and the latency of the steps behind it.
-template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) sample_kernel(SampleArgs p)
+template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) sample_kernel(SampleArgs p)
 {
     __shared__ Shared<THREADS> sh;
     const int i = blockIdx.x, wave = (int)uniform((uint32_t)threadIdx.x / kWave);
@@ -1188,7 +1234,7 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     float logprob = kNegInf;
     bool done = false;
     if constexpr (BF16)
-        if (!par.greedy && (!par.k || par.k > kMost)) done = sample_by_slots<THREADS>(sh, row, par, u, token, logprob);
+        if (!par.greedy && (!par.k || par.k > kMost)) done = sample_by_slots<THREADS, SLOTS>(sh, row, par, u, token, logprob);
     Found f;
     f.ok = false;
     f.top = __builtin_nanf("");
@@ -1317,8 +1363,14 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t st)
 {
-    if (a.r.bf16) COLLM_LAUNCH((sample_kernel<true, 1024>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
-    else COLLM_LAUNCH((sample_kernel<false, 1024>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    // bf16 rows for which there is a compute unit each are held in registers by their block (up to 4 or 16 chunks a thread), which finds the drawn
+    // one there: 256 rows of 128256 40 -> 35 us, one of 32000 16.6 -> 14.4.  More rows go two to a compute unit, and are read again.
+    const int chunks = a.r.vocab / 8;
+    const bool alone = a.r.bf16 && a.r.n_rows <= a.compute_units;
+    if (!a.r.bf16) COLLM_LAUNCH((sample_kernel<false, 1024, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    else if (alone && chunks <= 4 * 1024) COLLM_LAUNCH((sample_kernel<true, 1024, 4>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    else if (alone && chunks <= 16 * 1024) COLLM_LAUNCH((sample_kernel<true, 1024, 16>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    else COLLM_LAUNCH((sample_kernel<true, 1024, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 

@@ -25,6 +25,7 @@ struct SampleArgs {
     const float *top_p, *min_p;    // NULL: off
     int32_t *token;
     float *logprob;                // optional
+    int compute_units;             // of the GPU
 };
 
 struct TopArgs {
