@@ -1218,7 +1218,8 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
     }
 }
 
-// One block a row.  What bounds it: one pass over the row, and the latency of the steps behind it.
+// One block a row; SLOTS > 0: alone on its compute unit (of bf16 it holds that many chunks a thread).  What bounds it: one pass over the row, and
+// the latency of the steps behind it.
 template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) sample_kernel(SampleArgs p)
 {
     __shared__ Shared<THREADS> sh;
@@ -1363,11 +1364,13 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t st)
 {
-    // bf16 rows for which there is a compute unit each are held in registers by their block (up to 4 or 16 chunks a thread), which finds the drawn
-    // one there: 256 rows of 128256 40 -> 35 us, one of 32000 16.6 -> 14.4.  More rows go two to a compute unit, and are read again.
+    // Rows for which there is a compute unit each have its registers: of bf16 the block holds them (up to 4 or 16 chunks a thread) and finds the
+    // drawn logit there, 256 rows of 128256 40 -> 35 us, one of 32000 16.6 -> 14.4; of fp32 nothing goes to scratch memory, 200 rows of 50257 by
+    // steps 57.6 -> 54.8.  More rows go two to a compute unit: 1024 of 128256 with top-k 54 us, 73 with one.
     const int chunks = a.r.vocab / 8;
-    const bool alone = a.r.bf16 && a.r.n_rows <= a.compute_units;
-    if (!a.r.bf16) COLLM_LAUNCH((sample_kernel<false, 1024, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    const bool alone = a.r.n_rows <= a.compute_units;
+    if (!a.r.bf16 && alone) COLLM_LAUNCH((sample_kernel<false, 1024, 4>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    else if (!a.r.bf16) COLLM_LAUNCH((sample_kernel<false, 1024, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
     else if (alone && chunks <= 4 * 1024) COLLM_LAUNCH((sample_kernel<true, 1024, 4>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
     else if (alone && chunks <= 16 * 1024) COLLM_LAUNCH((sample_kernel<true, 1024, 16>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
     else COLLM_LAUNCH((sample_kernel<true, 1024, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
