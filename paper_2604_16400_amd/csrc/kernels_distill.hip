@@ -147,7 +147,7 @@ __device__ __forceinline__ Teacher read_record(const Record &rec, const DistillA
             if (rec.at[j] >= 0) part += exp2_neg(((double)rec.t[j] - ref) * (inv * log2e), 0);
         log_sum = log(wave_sum(part));
     }
-    const Exp by_tau(p.temperature, out.ref), plain(1.0f, out.ref);
+    const Exp<true> by_tau(p.temperature, out.ref), plain(1.0f, out.ref);  // (from the difference, whatever the logits' type)
     double p_sum = 0.0, entropy = 0.0, cross = 0.0, in = 0.0, in_ce = 0.0;
     bool twice = false;
     for (int j = lane; j < p.k; j += kWave) {
@@ -296,7 +296,7 @@ struct Finish {
 template <bool BF16, bool ONCE> struct Gradient {
     static constexpr int E = Row<BF16>::E;
     Coef c;
-    Exp by_tau, plain;
+    Exp<BF16> by_tau, plain;
     bool near, power, other;  // forms of the exponentials; whether there is a second term: a power of the first, or one of its own
     void *grad;
     bool same;  // its chunks lie as those of the logits
@@ -366,7 +366,7 @@ template <bool BF16, bool ONCE> struct Gradient {
     // at a place of the record: its logit, its probability
     __device__ __forceinline__ void entry(int at, float z, double prob, const DistillArgs &p, int label) const
     {
-        const Exp kd(p.temperature, c.max), ce(1.0f, c.max);
+        const Exp<BF16> kd(p.temperature, c.max), ce(1.0f, c.max);
         double g = (double)(c.in * kd(z)) - (double)c.kd * prob;
         if (c.ce != 0.0f) g += (double)(c.ce * ce(z)) - (at == label ? (double)c.label : 0.0);
         Elem<BF16>::store(grad, at, (float)g);
@@ -514,7 +514,7 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ vo
         Teacher t;
         if (wave == 0) t = read_record(rec, p, i, z_max, true, two);
         float ref = z_max > kNegInf ? z_max : 0.f;
-        const Exp by_tau(p.temperature, ref), plain(1.0f, ref);
+        const Exp<BF16> by_tau(p.temperature, ref), plain(1.0f, ref);
         float edge_out = edge_z;
         {
             const int e = row.whole * E + threadIdx.x;
@@ -555,8 +555,7 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ vo
         double drift = by_tau.drift(), drift_ce = other ? plain.drift() : 2.0 * drift;
         // finite, drifts that are roundings, and a rest that is not so small that the gradient would miss what was lost (3e-11 of the
         // record's largest term, times 2^32: it then is less than 1e-37 of the rest)
-        const bool near = rest > 0.125 && rest < 1e30 && rest_ce > 1e-15 && rest_ce < 1e30 && fabs(by_tau.drift() - 32.0) < 1.0 &&
-                          fabs(plain.drift() - 32.0) < 1.0;
+        const bool near = rest > 0.125 && rest < 1e30 && rest_ce > 1e-15 && rest_ce < 1e30 && by_tau.sound() && plain.sound();
         if (!near) {
             Running run;
             const float z[1] = {edge_out};

@@ -944,7 +944,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     if (threadIdx.x == 0) sh.count = sh.queued = 0;
     float top = fmaxf(edge_z, kNegInf), bound = kLow;
     double rest = 0.0;
-    Exp by_T(tau, 0.f);
+    Exp<BF16> by_T(tau, 0.f);
     auto largest = [&](const uint4 &v) {
         float m = kNegInf;
 #pragma unroll
@@ -972,7 +972,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     {
         // (what the sum is relative to: the largest of the first round)
         const float m = uniform(wave_max(sh.top[lane & (W - 1)]));
-        by_T = Exp(tau, m > kNegInf ? m : 0.f);
+        by_T = Exp<BF16>(tau, m > kNegInf ? m : 0.f);
     }
     int r = 0;
     for (int c = threadIdx.x; r * kRound < row.whole; ++r, c += kRound) {
@@ -1032,7 +1032,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     f.top = largest_logit;
     f.rest = rest * exp2_neg(-by_T.drift(), 0);
     f.ok = f.count <= kList && queued <= kQueue;
-    f.summed = rest < 1e30 && fabs(by_T.drift() - 32.0) < 1.0 && f.top < __builtin_huge_valf();
+    f.summed = rest < 1e30 && by_T.sound() && f.top < __builtin_huge_valf();
     return f;
 }
 
@@ -1247,7 +1247,7 @@ template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(T
     bool reaches = !done && f.ok && (!sums || f.summed) && (!par.k || f.count >= par.k || f.whole);
     if (reaches && sums && !f.whole) {
         // (what the list weighs, nearly: a list that cannot reach is not put in order)
-        const Exp by_T(par.T, f.ref);
+        const Exp<BF16> by_T(par.T, f.ref);
         double part = 0.0;
         for (int e = threadIdx.x; e < f.count; e += THREADS) part += (double)by_T(value_in(sh.listed[e]));
         part = block_sum<THREADS>(part, sh.red);

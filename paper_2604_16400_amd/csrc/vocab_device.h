@@ -164,15 +164,23 @@ template <bool ONCE> __device__ __forceinline__ uint4 load_chunk(__amdgpu_buffer
     return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(row, c * 16, 0, ONCE ? kOnce : 0));
 }
 
-// exp((z - ref) / tau).  near: 2^32 times that (what is below 2^-126 is lost: this is 2^-158 then), as exp2(z c + b) with b = 32 - ref c
-// rounded beforehand: the same factor 2^drift in every term, taken out in 64 bits.  Otherwise (ref too large for that) from the difference.
-// The rounding of c and of the argument are errors of |z - ref| / tau 2^-24 each, small where the result is not.
-struct Exp {
+// exp((z - ref) / tau).  The rounding of c and of the argument are errors of |z - ref| / tau 2^-24 each, small where the result is not.
+// near: 2^32 times that, for sums and gradients of a whole row; what is below 2^-126 is lost, 2^-158 here.  With bf16 logits it is exp2(z c + b), one
+// operation an element fewer than from the difference, with b = 32 - ref c rounded beforehand: the same factor 2^drift in every term, taken out
+// in 64 bits.  The argument is about 32 at the largest terms and rounded to 2^-20 there, an error of 7e-7: for fp32 logits it is the square
+// of an exponential of half the difference.
+template <bool BF16> struct Exp {
     float c, ref, b;
     __device__ __forceinline__ Exp(float tau, float r) : c(uniform((float)(1.44269504088896340736 / (double)tau))), ref(r), b(__builtin_fmaf(-r, c, 32.f)) {}
-    __device__ __forceinline__ float near(float z) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, c, b)); }
+    __device__ __forceinline__ float near(float z) const
+    {
+        if (BF16) return __builtin_amdgcn_exp2f(__builtin_fmaf(z, c, b));
+        const float half = __builtin_amdgcn_exp2f((z - ref) * (0.5f * c));
+        return half * 0x1p32f * half;
+    }
     __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z - ref) * c); }
-    __device__ __forceinline__ double drift() const { return (double)ref * (double)c + (double)b; }  // 32, about
+    __device__ __forceinline__ double drift() const { return BF16 ? (double)ref * (double)c + (double)b : 32.0; }  // 32, about
+    __device__ __forceinline__ bool sound() const { return fabs(drift() - 32.0) < 1.0; }                            // no more than rounding
 };
 
 // A thread's running sums: exp((z - m) / tau) and exp(z - m) over the logits it has met, m the largest of them
