@@ -1219,7 +1219,9 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
 }
 
 // One block a row; SLOTS > 0: alone on its compute unit (of bf16 it holds that many chunks a thread).  What bounds it: one pass over the row, and
-// the latency of the steps behind it.
+// the latency of the steps behind it; by value, the counters (2 to 3 logits a cycle and compute unit); by steps, the 64-bit weights (30 instructions a
+// logit).  Measured: 1024 x 128256 bf16 with top-k 20 54 us (4.9 TB/s), with top-p 0.9 102 (by value); 256 rows of them mixed 31; 200 x 50257 fp32 with top-p
+// 0.5 23 us (off the list), 0.9 55 (by steps); one row of 32000 bf16 8.3 greedy, 12.3 with top-k 50 and top-p, 14.3 with top-p alone.
 template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) sample_kernel(SampleArgs p)
 {
     __shared__ Shared<THREADS> sh;
@@ -1281,7 +1283,8 @@ template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(T
     }
 }
 
-// One block a row, as above; a list that is too long: by steps, the k-th place by counting, then the k logits up to it.
+// One block a row, two to a compute unit.  Bound by memory where there are many rows: 3277 x 128256 bf16, k 64, 179 us (4.7 TB/s); 205 x 50257 bf16, k 250,
+// 18 us; 32 x 32000 fp32, k 20, 12.3 us (one pass and a dozen block-wide waits).  A list that is too long: by steps, the k-th place by counting, then the k logits up to it.
 template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) top_kernel(TopArgs p)
 {
     __shared__ Shared<THREADS> sh;
