@@ -73,6 +73,11 @@ struct Weight {
     __device__ __forceinline__ u64 of(float z) const
     {
         if (top_inf) return z == __builtin_huge_valf() ? (u64)1 << scale : 0;
+        return finite(z);
+    }
+    // (where the largest logit is finite)
+    __device__ __forceinline__ u64 finite(float z) const
+    {
         // (added to 2^52, the last bit of the sum's fraction is worth 1: the rounding of that sum is the rounding)
         const double w = exp2_neg(((double)z - m) * c, scale) + 4503599627370496.0;
         return (u64)__double_as_longlong(w) & (((u64)1 << 52) - 1);
@@ -190,8 +195,16 @@ template <bool BF16, int THREADS> struct Steps {
     {
         each_value([&](float z, int idx) { f(key_of(z), idx); });
     }
-    // f(logit, index) over the row's logits, four loads on the way at any time
+    // f(logit, index) over the row's logits
     template <typename F> __device__ __forceinline__ void each_value(F f) const
+    {
+        each_chunk([&](const auto &z, int first) {
+#pragma unroll
+            for (int e = 0; e < (int)(sizeof z / sizeof z[0]); ++e) f(z[e], first + e);
+        });
+    }
+    // f(logits side by side, index of the first) over the row's chunks and, one by one, its edges; four loads on the way at any time
+    template <typename F> __device__ __forceinline__ void each_chunk(F f) const
     {
         constexpr int E = Row<BF16>::E, U = 4;
         const __amdgpu_buffer_rsrc_t from = row.buffer();
@@ -203,13 +216,18 @@ template <bool BF16, int THREADS> struct Steps {
             for (int u = 0; u < U; ++u) {
                 const int at = c + u * THREADS;
                 if (at < row.whole) {
+                    float z[E];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) f(Row<BF16>::value(v[u], e), row.lo + at * E + e);
+                    for (int e = 0; e < E; ++e) z[e] = Row<BF16>::value(v[u], e);
+                    f(z, row.lo + at * E);
                 }
                 v[u] = load_chunk<false>(from, at + U * THREADS);
             }
         }
-        if ((int)threadIdx.x < row.edges) f(row.edge(threadIdx.x), row.edge_index(threadIdx.x));
+        if ((int)threadIdx.x < row.edges) {
+            const float z[1] = {row.edge(threadIdx.x)};
+            f(z, row.edge_index(threadIdx.x));
+        }
     }
     __device__ __forceinline__ void clear(u64 *hist) const
     {
@@ -237,15 +255,32 @@ template <bool BF16, int THREADS> struct Steps {
         if (!(scale >= 0.f)) scale = 0.f;
         clear(sh.hist[0]);
     }
-    // The same of the weights of all logits; over: the sum of those of logits from `low` on that this thread met
+    // The same of the weights of all logits, the largest finite; of fp32 a chunk's are worked out side by
+    // side, without a branch (46 us of 200 rows of 50257 instead of 50; rows of bf16 rarely come here, and their kernel has no registers for it).  over: the sum of those of logits from `low` on that this thread met
     __device__ __forceinline__ u64 first_of_weights(float m, float lo, const Weight &w, float low, u64 &over)
     {
         begin(m, lo);
-        each_value([&](float z, int) {
-            if (!(z > kNegInf)) return;
-            const u64 x = w.of(z);
-            if (z >= low) over += x;
-            if (x) atomicAdd(&sh.hist[0][step_of(z)], x);
+        if constexpr (BF16) {
+            each_value([&](float z, int) {
+                if (!(z > kNegInf)) return;
+                const u64 x = w.finite(z);
+                if (z >= low) over += x;
+                if (x) atomicAdd(&sh.hist[0][step_of(z)], x);
+            });
+        }
+        else each_chunk([&](const auto &z, int) {
+            constexpr int N = (int)(sizeof z / sizeof z[0]);
+            u64 x[N], any = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                x[e] = w.finite(z[e]);
+                if (!(z[e] > kNegInf)) x[e] = 0;
+                over += z[e] >= low ? x[e] : 0;
+                any |= x[e];
+            }
+            if (!any) return;
+#pragma unroll
+            for (int e = 0; e < N; ++e) atomicAdd(&sh.hist[0][step_of(z[e])], x[e]);
         });
         __syncthreads();
         scan = Scan<THREADS>(sh, sh.hist[0]);
@@ -461,7 +496,7 @@ __device__ __forceinline__ void sample_by_steps(Shared<THREADS> &sh, const Row<B
     }
     u64 over = 0;
     const float end = fmaxf(least, m - 44.0f * par.T);
-    const bool all = last == ~(u64)0;
+    const bool all = last == ~(u64)0 && !w.top_inf;
     u64 total;
     if (all) {
         total = steps.first_of_weights(m, end, w, key_min > kKeyNone ? value_of(key_min) : kNegInf, over);
@@ -502,14 +537,34 @@ __device__ __forceinline__ void sample_by_steps(Shared<THREADS> &sh, const Row<B
     float draw_least, draw_most, cut_least = __builtin_huge_valf(), cut_most = kNegInf;
     steps.bounds(bin_1, bin_2, draw_least, draw_most);
     if (cut_bin >= 0) steps.bounds(cut_bin, cut_bin, cut_least, cut_most);
-    steps.each_value([&](float z, int idx) {
-        if (!((z >= draw_least && z <= draw_most) || (z >= cut_least && z <= cut_most)) || !(z > kNegInf)) return;
+    auto may_be = [&](float z) { return (z >= draw_least && z <= draw_most) || (z >= cut_least && z <= cut_most); };
+    auto list = [&](float z, int idx) {
+        if (!(z > kNegInf)) return;
         const uint32_t key = key_of(z);
         const int b = steps.step(key);
         if (((b < bin_1 || b > bin_2) && b != cut_bin) || entry(key, idx) > last) return;
         const int to = atomicAdd(&sh.count, 1);
         if (to < kList) sh.listed[to] = entry(key, idx);
-    });
+    };
+    if constexpr (BF16) {
+        steps.each_value([&](float z, int idx) {
+            if (may_be(z)) list(z, idx);
+        });
+    } else {
+        steps.each_chunk([&](const auto &z, int first) {
+            constexpr int N = (int)(sizeof z / sizeof z[0]);
+            bool any = false, in[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                in[e] = (z[e] >= draw_least & z[e] <= draw_most) | (z[e] >= cut_least & z[e] <= cut_most);
+                any |= in[e];
+            }
+            if (!any) return;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (in[e]) list(z[e], first + e);
+        });
+    }
     __syncthreads();
     const int count = (int)uniform((uint32_t)sh.count);
     if (count <= kList && sort_list<THREADS>(sh, count)) {
@@ -1221,7 +1276,7 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
 // One block a row; SLOTS > 0: alone on its compute unit (of bf16 it holds that many chunks a thread).  What bounds it: one pass over the row, and
 // the latency of the steps behind it; by value, the counters (2 to 3 logits a cycle and compute unit); by steps, the 64-bit weights (30 instructions a
 // logit).  Measured: 1024 x 128256 bf16 with top-k 20 54 us (4.9 TB/s), with top-p 0.9 102 (by value); 256 rows of them mixed 31; 200 x 50257 fp32 with top-p
-// 0.5 23 us (off the list), 0.9 55 (by steps); one row of 32000 bf16 8.3 greedy, 12.3 with top-k 50 and top-p, 14.3 with top-p alone.
+// 0.5 23 us (off the list), 0.9 50 (by steps); one row of 32000 bf16 8.3 greedy, 12.3 with top-k 50 and top-p, 14.3 with top-p alone.
 template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) sample_kernel(SampleArgs p)
 {
     __shared__ Shared<THREADS> sh;
