@@ -5,6 +5,7 @@ import math
 
 import numpy as np
 import pytest
+from test_gpu_vocab import _distill_case, _sample_case, _top_case
 
 from oracle import vocab as ov
 from paper_2604_16400_amd import binding as b
@@ -101,3 +102,13 @@ def test_both_marshalling_routes_give_the_same_call(monkeypatch):
     monkeypatch.setattr(b, "_marshal", None)
     for x, y in zip(first, everything()):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_vocabulary(dtype):
+    """2^20 words and a record of 1024: the most shared memory a call asks for, the fewest bits of a weight."""
+    V = 1 << 20
+    _sample_case(V, dtype, 1, n=6)
+    _top_case(V, dtype, 1024, 1.0, 2, n=3)
+    for how, workspace in (("loss", False), ("step", False), ("step", True), ("two", False)):
+        _distill_case(V, dtype, 1024, 2.0, True, True, 3, how, workspace=workspace, n=3)
