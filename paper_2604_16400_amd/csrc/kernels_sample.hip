@@ -1352,9 +1352,14 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     double sum = 0.0;  // of exp((z - ref) / temperature)
     bool sorted = f.ok && (f.count >= p.k || f.whole) && sort_list<THREADS>(sh, f.count);
     if (p.lse && sorted && f.summed) {
+        // (relative to the row's largest logit, which may lie any distance above what the rest is summed relative to)
         const double c = 1.44269504088896340736 / (double)p.temperature;
         for (int e = threadIdx.x; e < f.count; e += THREADS)
-            sum += exp2_neg(((double)value_in(sh.listed[e]) - (double)f.ref) * c, 0);
+            sum += exp2_neg(((double)value_in(sh.listed[e]) - (double)f.top) * c, 0);
+        if (f.count > 0) {
+            f.rest *= exp2_neg(((double)f.ref - (double)f.top) * c, 0);
+            f.ref = f.top;
+        }
     }
     if (p.lse && !(sorted && f.summed)) {
         // (relative to each thread's largest logit; of the logits as they are: a NaN among them shows, also beside +inf)
