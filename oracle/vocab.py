@@ -41,6 +41,31 @@ def sample(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     return int(o[at]), float(np.log(w[at] / run[-1]))
 
 
+def sample_whole(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """The same by weights rounded to whole multiples of 2^-45 (2^(log2 rows - 62) for long rows), which settle ties at a border beside a tail that weighs
+    next to nothing.  Finite logits, -inf and NaN; temperature 0 or above 0 and finite.  (Weights next to half a unit, of which an exponential's last
+    bits decide, are the caller's to keep away.)"""
+    z, (u, temperature, top_p, min_p) = np.asarray(z, np.float64), (float(np.float32(v)) for v in (u, temperature, top_p, min_p))
+    o = order(z)
+    if not len(o):
+        return -1, -np.inf
+    if not temperature > 0:
+        return int(o[0]), 0.0
+    y = (z[o] - z[o[0]]) / temperature
+    scale = min(45, 62 - int(len(z)).bit_length())
+    w = np.rint(np.ldexp(np.exp(y), scale)).astype(np.int64)
+    if top_k > 0:
+        w = w[:top_k]
+    run, n = np.cumsum(w), len(w)
+    if top_p < 1:
+        n = max(1, int(np.searchsorted(run - w, int(np.ceil(top_p * float(run[-1]))))))
+    if min_p > 0:
+        n = min(n, int(np.count_nonzero(y >= np.log(min(min_p, 1.0)))))
+    kept = int(run[n - 1])
+    at = int(np.searchsorted(run, min(int(u * float(kept)), kept - 1), side="right"))
+    return int(o[at]), float(y[at] - np.log(np.ldexp(float(kept), -scale)))
+
+
 def top(z, k, temperature=1.0):
     """(values [k], indices [k], log-sum-exp of z / temperature); -inf and -1 behind the last logit above -inf."""
     z = np.asarray(z, np.float64)

@@ -966,7 +966,7 @@ struct Found {
     int count;    // listed
     bool whole;   // every logit above -inf is listed
     double rest;  // sum of exp((z - ref) / T) over what is not listed
-    float ref, top;  // what the sum is relative to; the largest logit
+    float ref, top;  // what the sum is relative to, at most the largest logit (0 where all are -inf); the largest logit
     bool ok;      // the list is not too long (and what it is sorted by is a number)
     bool summed;  // `rest` is right but for 2^-17 of it
 };
@@ -1024,14 +1024,23 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
         if (lane == 0) sh.top[wave] = m;
     }
     raise_bound();
-    {
-        // (what the sum is relative to: the largest of the first round)
-        const float m = uniform(wave_max(sh.top[lane & (W - 1)]));
-        by_T = Exp<BF16>(tau, m > kNegInf ? m : 0.f);
-    }
+    // What the sum is relative to: the largest of the first round, or, where that is all -inf, of the rounds up to the first with another logit.  As long as
+    // there is none the bound is below every finite logit, so nothing but -inf has been added.
+    float first = uniform(wave_max(sh.top[lane & (W - 1)]));
+    auto refer = [&]() { by_T = Exp<BF16>(tau, first > kNegInf ? first : 0.f); };
+    refer();
     int r = 0;
     for (int c = threadIdx.x; r * kRound < row.whole; ++r, c += kRound) {
-        if (r > 1) raise_bound();  // (of the second round nothing is known yet)
+        if (r > 1) {  // (of the second round nothing is known yet)
+            raise_bound();
+            if (sums && !(first > kNegInf)) {
+                const float m = wave_max(top);
+                if (lane == 0) sh.top[wave] = m;
+                __syncthreads();
+                first = uniform(wave_max(sh.top[lane & (W - 1)]));
+                refer();
+            }
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = c + u * THREADS;
@@ -1061,6 +1070,10 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     if (r > 1) raise_bound();
     else __syncthreads();
     const float largest_logit = uniform(wave_max(sh.all[lane & (W - 1)]));
+    if (!(first > kNegInf)) {
+        first = largest_logit;
+        refer();
+    }
     // everything from the last bound on is listed
     auto look_at = [&](float z, int idx) {
         if (z >= bound) {
