@@ -1016,31 +1016,30 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
         bound = uniform(fmaxf(-wave_max(-sh.low[turn][lane & (W - 1)]), kLow));
         turn ^= 1;
     };
+    // What the sum is relative to: the largest of the first round that is not all -inf.  Rounds before that one (`none` of them) weigh nothing whatever
+    // it is; a NaN in them shows in the sum.
+    int none = 0;
+    for (;; ++none) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (u * THREADS + (int)threadIdx.x < row.whole) top = fmaxf(top, largest(v[u]));
-    {
+        for (int u = 0; u < U; ++u)
+            if (none * kRound + u * THREADS + (int)threadIdx.x < row.whole) top = fmaxf(top, largest(v[u]));
         const float m = wave_max(top);
         if (lane == 0) sh.top[wave] = m;
-    }
-    raise_bound();
-    // What the sum is relative to: the largest of the first round, or, where that is all -inf, of the rounds up to the first with another logit.  As long as
-    // there is none the bound is below every finite logit, so nothing but -inf has been added.
-    float first = uniform(wave_max(sh.top[lane & (W - 1)]));
-    auto refer = [&]() { by_T = Exp<BF16>(tau, first > kNegInf ? first : 0.f); };
-    refer();
-    int r = 0;
-    for (int c = threadIdx.x; r * kRound < row.whole; ++r, c += kRound) {
-        if (r > 1) {  // (of the second round nothing is known yet)
-            raise_bound();
-            if (sums && !(first > kNegInf)) {
-                const float m = wave_max(top);
-                if (lane == 0) sh.top[wave] = m;
-                __syncthreads();
-                first = uniform(wave_max(sh.top[lane & (W - 1)]));
-                refer();
-            }
+        raise_bound();
+        const float first = uniform(wave_max(sh.top[lane & (W - 1)]));
+        if (first > kNegInf) by_T.refer(first);
+        if (first > kNegInf || !sums || (none + 1) * kRound >= row.whole) break;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) rest += (double)by_T.near(Row<BF16>::value(v[u], e));
+            v[u] = load_chunk<false>(from, (none + 1) * kRound + u * THREADS + threadIdx.x);
         }
+        __syncthreads();  // (sh.top has been read)
+    }
+    int r = none;
+    for (int c = r * kRound + threadIdx.x; r * kRound < row.whole; ++r, c += kRound) {
+        if (r > none + 1) raise_bound();  // (of the next round nothing is known yet)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = c + u * THREADS;
@@ -1067,13 +1066,9 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
         const float m = wave_max(top);
         if (lane == 0) sh.all[wave] = m;
     }
-    if (r > 1) raise_bound();
+    if (r > none + 1) raise_bound();
     else __syncthreads();
     const float largest_logit = uniform(wave_max(sh.all[lane & (W - 1)]));
-    if (!(first > kNegInf)) {
-        first = largest_logit;
-        refer();
-    }
     // everything from the last bound on is listed
     auto look_at = [&](float z, int idx) {
         if (z >= bound) {
@@ -1365,14 +1360,14 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
     double sum = 0.0;  // of exp((z - ref) / temperature)
     bool sorted = f.ok && (f.count >= p.k || f.whole) && sort_list<THREADS>(sh, f.count);
     if (p.lse && sorted && f.summed) {
-        // (relative to the row's largest logit, which may lie any distance above what the rest is summed relative to)
-        const double c = 1.44269504088896340736 / (double)p.temperature;
-        for (int e = threadIdx.x; e < f.count; e += THREADS)
-            sum += exp2_neg(((double)value_in(sh.listed[e]) - (double)f.top) * c, 0);
-        if (f.count > 0) {
-            f.rest *= exp2_neg(((double)f.ref - (double)f.top) * c, 0);
+        // (relative to the row's largest logit where that lies so far above `ref` that the terms would leave the range)
+        const double c = 1.44269504088896340736 / (double)p.temperature, above = ((double)f.top - (double)f.ref) * c;
+        if (above > 512.0) {
+            f.rest *= exp2_neg(-above, 0);
             f.ref = f.top;
         }
+        for (int e = threadIdx.x; e < f.count; e += THREADS)
+            sum += exp2_neg(((double)value_in(sh.listed[e]) - (double)f.ref) * c, 0);
     }
     if (p.lse && !(sorted && f.summed)) {
         // (relative to each thread's largest logit; of the logits as they are: a NaN among them shows, also beside +inf)

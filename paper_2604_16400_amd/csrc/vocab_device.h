@@ -172,6 +172,11 @@ template <bool ONCE> __device__ __forceinline__ uint4 load_chunk(__amdgpu_buffer
 template <bool BF16> struct Exp {
     float c, ref, b;
     __device__ __forceinline__ Exp(float tau, float r) : c(uniform((float)(1.44269504088896340736 / (double)tau))), ref(r), b(__builtin_fmaf(-r, c, 32.f)) {}
+    __device__ __forceinline__ void refer(float r)  // to another reference
+    {
+        ref = r;
+        b = __builtin_fmaf(-r, c, 32.f);
+    }
     __device__ __forceinline__ float near(float z) const
     {
         if (BF16) return __builtin_amdgcn_exp2f(__builtin_fmaf(z, c, b));
