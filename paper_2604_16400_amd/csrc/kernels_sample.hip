@@ -1190,10 +1190,11 @@ template <int THREADS> __device__ __forceinline__ bool sort_list(Shared<THREADS>
     return true;
 }
 
-// What a list in order says, by one wave: sh.drawn whether it decides the row, sh.bin the token, sh.logprob.  rest: sum of the weights that are
-// not listed, good to 2^-17 of it; whole: there are none.
+// What a list in order says, by one wave: sh.drawn whether it decides the row, sh.bin the token, sh.logprob.  rest: sum of the exponentials that are
+// not listed, good to 2^-17 of it; unlisted: how many they are, at most (0: none).  The weights are whole numbers: each of those not listed is
+// within half a unit of its exponential.  What comes out has to be the same for every sum in between.
 template <int THREADS>
-__device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par, float u, const Weight &w, int count, double rest, bool whole)
+__device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par, float u, const Weight &w, int count, double rest, int unlisted)
 {
     const int lane = threadIdx.x & (kWave - 1);
     // lane l has entries each * l ..; their weights beside them
@@ -1213,19 +1214,25 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
         if (lane >= o) incl += up;
     }
     const u64 first = incl - sum, listed = uniform((u64)__shfl(incl, kWave - 1));
-    // what all weights sum to, at least and at most
-    const double all[2] = {(double)listed + rest * (1.0 - 0x1p-17), (double)listed + rest * (1.0 + 0x1p-17)};
+    // what all weights sum to, at least and at most (a few roundings of the sums here beside the rest's)
+    double all[2] = {(double)listed, (double)listed};
+    if (unlisted) {
+        const double unit = 0.5 * (double)unlisted + 0x1p-50 * (all[0] + rest);
+        all[0] = fmax(all[0], all[0] + rest * (1.0 - 0x1p-17) - unit);
+        all[1] += rest * (1.0 + 0x1p-17) + unit;
+    }
     // the first entries that the cuts leave out
     int cut[2] = {n_k, n_k}, cut_m = n_k;
     if (par.top_p < 1.0f || par.min_p > 0.0f) {
         const double low = min_p_logit(w, par);
+        const u64 goal[2] = {(u64)ceil(fmax((double)par.top_p * all[0], 0.0)), (u64)ceil(fmax((double)par.top_p * all[1], 0.0))};
         u64 before = first;
 #pragma nounroll
         for (int e = begin; e < end; ++e) {
             if (e > 0 && par.top_p < 1.0f) {
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
-                    if (e < cut[a] && (double)before >= (double)par.top_p * all[a]) cut[a] = e;
+                    if (e < cut[a] && before >= goal[a]) cut[a] = e;
             }
             if (e < cut_m && par.min_p > 0.0f && (double)value_in(sh.listed[e]) < low) cut_m = e;
             before += sh.binned[e];
@@ -1239,7 +1246,7 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
     }
     const int n = cut[0] < cut_m ? cut[0] : cut_m;
     // the list has to reach the cut: as the end of the top-k, of the row, or because something cuts before its end (for certain)
-    const bool ends = n < n_k || par.k || whole;
+    const bool ends = n < n_k || par.k || !unlisted;
     const bool open = !ends && !(par.top_p < 1.0f) && !(par.min_p > 0.0f);  // nothing cuts at all
     bool decides = (ends || open) && (cut[0] == cut[1] || n < cut[0]);
     u64 kept = 0;
@@ -1329,7 +1336,7 @@ template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(T
             const Weight w = weight_of(m, par.T, row.n);
             // what the row's weights beside the list sum to
             const double rest = sums ? f.rest * exp2_neg(((double)f.ref - (double)m) * w.c, w.scale) : 0.0;
-            if (wave == 0) read_list(sh, par, u, w, f.count, rest, f.whole);
+            if (wave == 0) read_list(sh, par, u, w, f.count, rest, sums && !f.whole ? row.n - f.count : 0);
             __syncthreads();
             done = uniform((uint32_t)sh.drawn) != 0;
             token = sh.bin;
