@@ -78,6 +78,18 @@ int check_grad(const collm_logits *s, const void *logits, const float *dloss, co
     return apart || (z == g && s->ld == ld_grad) ? COLLM_OK : COLLM_E_SHAPE;
 }
 
+// the call's rows, as many at a time as a launch takes
+template <typename Args> int launch_rows(const Args &a, hipError_t (*launch)(const Args &, hipStream_t), void *stream)
+{
+    for (int64_t first = 0; first < a.r.n_rows; first += kLaunchRows) {
+        const int64_t left = a.r.n_rows - first;
+        Args part = a;
+        part.take((int)first, (int)(left < kLaunchRows ? left : kLaunchRows));
+        HIP_TRY(launch(part, (hipStream_t)stream));
+    }
+    return COLLM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -104,8 +116,7 @@ int collm_sample(int device, const collm_logits *shape, const void *logits, cons
     a.logprob = logprob;
     HIP_TRY(hipSetDevice(device));
     HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
-    HIP_TRY(launch_sample(a, (hipStream_t)stream));
-    return COLLM_OK;
+    return launch_rows(a, launch_sample, stream);
 }
 
 int collm_top_logits(int device, const collm_logits *shape, const void *logits, int32_t k, float temperature, float *values, int32_t *indices,
@@ -125,8 +136,7 @@ int collm_top_logits(int device, const collm_logits *shape, const void *logits, 
     a.indices = indices;
     a.lse = lse;
     HIP_TRY(hipSetDevice(device));
-    HIP_TRY(launch_top_logits(a, (hipStream_t)stream));
-    return COLLM_OK;
+    return launch_rows(a, launch_top_logits, stream);
 }
 
 int collm_distill_fwd(int device, const collm_logits *shape, const void *logits, const collm_distill *teacher, float *loss, float *stats,
@@ -142,8 +152,7 @@ int collm_distill_fwd(int device, const collm_logits *shape, const void *logits,
     a.stats = stats;
     HIP_TRY(hipSetDevice(device));
     HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
-    HIP_TRY(launch_distill_fwd(a, (hipStream_t)stream));
-    return COLLM_OK;
+    return launch_rows(a, launch_distill_fwd, stream);
 }
 
 int collm_distill_bwd(int device, const collm_logits *shape, const void *logits, const collm_distill *teacher, const float *stats, const float *dloss,
@@ -161,8 +170,7 @@ int collm_distill_bwd(int device, const collm_logits *shape, const void *logits,
     a.ld_grad = ld_grad;
     HIP_TRY(hipSetDevice(device));
     HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
-    HIP_TRY(launch_distill_bwd(a, (hipStream_t)stream));
-    return COLLM_OK;
+    return launch_rows(a, launch_distill_bwd, stream);
 }
 
 int collm_distill_fwd_bwd(int device, const collm_logits *shape, const void *logits, const collm_distill *teacher, const float *dloss, float *loss,
@@ -183,8 +191,7 @@ int collm_distill_fwd_bwd(int device, const collm_logits *shape, const void *log
     a.workspace_bytes = workspace_bytes;
     HIP_TRY(hipSetDevice(device));
     HIP_TRY(hipDeviceGetAttribute(&a.compute_units, hipDeviceAttributeMultiprocessorCount, device));
-    HIP_TRY(launch_distill_fwd_bwd(a, (hipStream_t)stream));
-    return COLLM_OK;
+    return launch_rows(a, launch_distill_fwd_bwd, stream);
 }
 
 }  // extern "C"

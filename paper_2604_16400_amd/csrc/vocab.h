@@ -1,4 +1,5 @@
-// Argument blocks and launchers of the vocabulary operators (kernels_sample.hip, kernels_distill.hip).
+// Argument blocks and launchers of the vocabulary operators (kernels_sample.hip, kernels_distill.hip).  take(first, n) leaves `n` rows of a call, from row
+// `first` on.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -7,6 +8,9 @@ namespace collm {
 
 constexpr int kMaxVocab = 1 << 20;  // columns of a row of logits (a bitmap of a row fits the LDS; fixed-point sums have 20 bits to grow)
 constexpr int kMaxTop = 1024;       // entries of a teacher's record
+constexpr int kDistillStats = 8;    // floats that a forward call keeps of a row for the backward call
+constexpr int kLaunchRows = 1 << 21;  // rows of one launch at most: a block of up to 1024 threads each, and a grid has fewer than 2^32
+static_assert((int64_t)kLaunchRows * 1024 < (int64_t)1 << 32, "threads of a grid");
 
 // The rows of one call: row i of the call is row (rows ? rows[i] : i) of the logits; an entry of `rows` outside
 // [0, n_held) is a row that is not there
@@ -16,7 +20,23 @@ struct LogitRows {
     const int32_t *rows;
     int n_rows, n_held, vocab;
     bool bf16;
+    void take(int first, int n)
+    {
+        n_rows = n;
+        if (rows) {
+            rows += first;
+        } else {
+            logits = (const char *)logits + first * ld * (bf16 ? 2 : 4);
+            n_held -= first;
+        }
+    }
 };
+
+// past the entries of `rows` rows, `width` each, of an array (NULL: there is none)
+template <typename T> void skip(T *&p, int64_t rows, int64_t width = 1)
+{
+    if (p) p += rows * width;
+}
 
 struct SampleArgs {
     LogitRows r;
@@ -26,6 +46,11 @@ struct SampleArgs {
     int32_t *token;
     float *logprob;                // optional
     int compute_units;             // of the GPU
+    void take(int first, int n)
+    {
+        r.take(first, n);
+        skip(u, first), skip(temperature, first), skip(top_k, first), skip(top_p, first), skip(min_p, first), skip(token, first), skip(logprob, first);
+    }
 };
 
 struct TopArgs {
@@ -35,10 +60,12 @@ struct TopArgs {
     float *values;     // [n_rows, k]
     int32_t *indices;  // [n_rows, k]
     float *lse;        // optional
+    void take(int first, int n)
+    {
+        r.take(first, n);
+        skip(values, first, k), skip(indices, first, k), skip(lse, first);
+    }
 };
-
-// floats that a forward call keeps of a row for the backward call
-constexpr int kDistillStats = 8;
 
 struct DistillArgs {
     LogitRows r;
@@ -56,6 +83,13 @@ struct DistillArgs {
     int compute_units;        // of the GPU
     void *workspace;          // of the call that does both
     int64_t workspace_bytes;
+    void take(int first, int n)
+    {
+        r.take(first, n);
+        skip(t_values, first, k), skip(t_indices, first, k), skip(t_lse, first), skip(labels, first);
+        skip(loss, first), skip(stats, first, kDistillStats), skip(dloss, first);
+        if (dlogits && !r.rows) dlogits = (char *)dlogits + first * ld_grad * (r.bf16 ? 2 : 4);
+    }
 };
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t st);
