@@ -523,29 +523,38 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ vo
         }
         // over the rest of the row: sums of exp((z - ref) / tau) and, for the label at another temperature, of exp(z - ref); at temperature
         // 2 the latter is the former's square
-        float part = by_tau.near(edge_out), part_ce = other ? plain.near(edge_out) : part * part;
+        double part, part_ce;  // (a chunk's terms in 32 bits, chunks in 64)
+        {
+            const float u = by_tau.near(edge_out);
+            part = (double)u;
+            part_ce = (double)(other ? plain.near(edge_out) : u * u);
+        }
         held.each(row, [&](uint4 &v, int k, auto) {
             if (tail) mask_chunk<BF16>(v, bits, k);
+            float s = 0.f, s_ce = 0.f;
             if (other) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    part += by_tau.near(Row<BF16>::value(v, e));
-                    part_ce += plain.near(Row<BF16>::value(v, e));
+                    s += by_tau.near(Row<BF16>::value(v, e));
+                    s_ce += plain.near(Row<BF16>::value(v, e));
                 }
+                part_ce += (double)s_ce;
             } else if (two) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const float u = by_tau.near(Row<BF16>::value(v, e));
-                    part += u;
-                    part_ce = __builtin_fmaf(u, u, part_ce);
+                    s += u;
+                    s_ce = __builtin_fmaf(u, u, s_ce);
                 }
+                part_ce += (double)s_ce;
             } else {
 #pragma unroll
-                for (int e = 0; e < E; ++e) part += by_tau.near(Row<BF16>::value(v, e));
+                for (int e = 0; e < E; ++e) s += by_tau.near(Row<BF16>::value(v, e));
             }
+            part += (double)s;
         });
         load_logits(next_row);
-        double rest = wave_sum((double)part), rest_ce = two ? wave_sum((double)part_ce) : 1.0;
+        double rest = wave_sum(part), rest_ce = two ? wave_sum(part_ce) : 1.0;
         if (lane == 0) {
             sh.sum[wave] = rest;
             sh.sum_ce[wave] = rest_ce;
@@ -571,8 +580,8 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ vo
             __syncthreads();
             const float m = wave_max(run.m);
             run.raise(m, by_tau.c);
-            rest = wave_sum((double)run.s);
-            rest_ce = wave_sum((double)run.ce);
+            rest = wave_sum(run.s);
+            rest_ce = wave_sum(run.ce);
             if (lane == 0) {
                 sh.max[wave] = m;
                 sh.sum[wave] = rest;
@@ -766,7 +775,7 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS) dis
     }
     const float m = wave_max(run.m);
     run.raise(m, c);
-    const double s = wave_sum((double)run.s), ce = wave_sum((double)run.ce);
+    const double s = wave_sum(run.s), ce = wave_sum(run.ce);
     if (lane == 0) {
         sh.max[wave] = m;
         sh.sum[wave] = s;

@@ -1394,7 +1394,7 @@ template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) 
         }
         f.ref = block_max<THREADS>(run.m, sh.red);
         run.raise(f.ref, c);
-        sum = f.ref < __builtin_huge_valf() ? (double)run.s : nan ? __builtin_nan("") : __builtin_huge_val();
+        sum = f.ref < __builtin_huge_valf() ? run.s : nan ? __builtin_nan("") : __builtin_huge_val();
         f.rest = 0.0;
     }
     if (p.lse) {

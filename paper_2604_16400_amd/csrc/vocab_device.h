@@ -188,14 +188,16 @@ template <bool BF16> struct Exp {
     __device__ __forceinline__ bool sound() const { return fabs(drift() - 32.0) < 1.0; }                            // no more than rounding
 };
 
-// A thread's running sums: exp((z - m) / tau) and exp(z - m) over the logits it has met, m the largest of them
+// A thread's running sums: exp((z - m) / tau) and exp(z - m) over the logits it has met, m the largest of them.  A chunk's terms are added in 32
+// bits, chunks in 64: in 32 the roundings of a long sum of like terms all go one way (3e-5 after 4096 chunks).
 struct Running {
-    float m = kLow, s = 0.f, ce = 0.f;
+    float m = kLow;
+    double s = 0.0, ce = 0.0;
     // (to a larger reference)
     __device__ __forceinline__ void raise(float to, float c)
     {
-        s *= __builtin_amdgcn_exp2f((m - to) * c);
-        ce *= __builtin_amdgcn_exp2f((m - to) * 1.44269504f);
+        s *= (double)__builtin_amdgcn_exp2f((m - to) * c);
+        ce *= (double)__builtin_amdgcn_exp2f((m - to) * 1.44269504f);
         m = to;
     }
     template <int N> __device__ __forceinline__ void add(const float (&z)[N], float c)
@@ -204,11 +206,14 @@ struct Running {
 #pragma unroll
         for (int e = 0; e < N; ++e) top = fmaxf(top, z[e]);
         raise(top, c);
+        float part = 0.f, part_ce = 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            s += __builtin_amdgcn_exp2f((z[e] - m) * c);
-            ce += __builtin_amdgcn_exp2f((z[e] - m) * 1.44269504f);
+            part += __builtin_amdgcn_exp2f((z[e] - m) * c);
+            part_ce += __builtin_amdgcn_exp2f((z[e] - m) * 1.44269504f);
         }
+        s += (double)part;
+        ce += (double)part_ce;
     }
 };
 
