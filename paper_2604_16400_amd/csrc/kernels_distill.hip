@@ -179,6 +179,7 @@ __device__ __forceinline__ Teacher read_record(const Record &rec, const DistillA
         out.in_ce = two ? wave_sum(in_ce) : out.in;
     }
     if (__any(twice)) {
+        wave_sync();
         for (int j = lane; j < p.k; j += kWave) {
             double q = 0.0;
             if (rec.first[j])
@@ -186,6 +187,7 @@ __device__ __forceinline__ Teacher read_record(const Record &rec, const DistillA
                     if (rec.at[l] == rec.at[j]) q += rec.p[l];
             rec.t[j] = (float)q;  // (the record's t is not needed any more)
         }
+        wave_sync();
         for (int j = lane; j < p.k; j += kWave) rec.p[j] = (double)rec.t[j];
     }
     return out;
@@ -602,7 +604,10 @@ template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ vo
             // (the loss itself while the other waves go on)
             const double loss = end.loss(p, label_z);
             if (lane == 0) p.loss[i] = (float)loss;
-            if (p.stats && lane < kDistillStats) p.stats[(int64_t)i * kDistillStats + lane] = sh.coef[lane];
+            if (p.stats) {
+                if (!GRAD) wave_sync();
+                if (lane < kDistillStats) p.stats[(int64_t)i * kDistillStats + lane] = sh.coef[lane];
+            }
         } else if (GRAD) {
             __syncthreads();
         }

@@ -142,6 +142,14 @@ __device__ __forceinline__ double exp2_neg(double t, int scale)
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kLow = -3.402823466e+38f;  // the least finite value: a running maximum begins here, so that -inf adds nothing
 
+// Between writes to shared memory by a wave's lanes and reads of them by other lanes of that wave (and the other way round)
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
 template <typename T, typename F> __device__ __forceinline__ T wave_reduce(T v, F f)
 {
 #pragma unroll
