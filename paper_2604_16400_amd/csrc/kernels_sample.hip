@@ -103,7 +103,7 @@ template <int THREADS> struct Shared {
     int bins[2];
     uint32_t key_min, key_max;
     int bin;
-    int count, queued;
+    int count, queued, beyond;
     int cut_m, drawn;
     float logprob;
     u64 kept;
@@ -996,7 +996,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = load_chunk<false>(from, u * THREADS + threadIdx.x);
-    if (threadIdx.x == 0) sh.count = sh.queued = 0;
+    if (threadIdx.x == 0) sh.count = sh.queued = sh.beyond = 0;
     float top = fmaxf(edge_z, kNegInf), bound = kLow;
     double rest = 0.0;
     Exp<BF16> by_T(tau, 0.f);
@@ -1069,25 +1069,38 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     if (r > none + 1) raise_bound();
     else __syncthreads();
     const float largest_logit = uniform(wave_max(sh.all[lane & (W - 1)]));
-    // everything from the last bound on is listed
-    auto look_at = [&](float z, int idx) {
+    // Everything from the last bound on is listed.  The rest is added up in whole units, 2^-41 or less of the largest it may hold: which thread looks at which of
+    // the chunks put aside is a matter of the run, and whole numbers have the same sum in every order.  A thread has at most 2^10 logits, so
+    // 2^51 units and their roundings; sh.beyond: somewhere it has more, or no number.
+    const int power = (int)(__float_as_uint(fminf(fmaxf(by_T.near(bound), 0x1p-100f), 1e30f)) >> 23) - 126;  // (2 to it is above that)
+    const double scale = __builtin_ldexp(1.0, 41 - power);
+    u64 units = 0;
+    auto add = [&](double sum) {
+        const double x = sum * scale;
+        if (x < 0x1.4p51) units += (u64)__double_as_longlong(x + 0x1p52) & (((u64)1 << 52) - 1);
+        else sh.beyond = 1;
+    };
+    auto look_at = [&](float z, int idx, double &sum) {
         if (z >= bound) {
             const int to = atomicAdd(&sh.count, 1);
             if (to < kList) sh.listed[to] = entry(key_of(z), idx);
         } else if (sums) {
-            rest += (double)by_T.near(z);
+            sum += (double)by_T.near(z);
         }
     };
-    look_at(edge_z, row.edge_index(threadIdx.x));
+    look_at(edge_z, row.edge_index(threadIdx.x), rest);
+    if (sums) add(rest);
     const int queued = (int)uniform((uint32_t)sh.queued);
     for (int q = threadIdx.x; q < (queued < kQueue ? queued : kQueue); q += THREADS) {
         const uint4 chunk = sh.chunk[q];
         const int first = row.lo + sh.chunk_at[q] * E;
+        double part = 0.0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) look_at(Row<BF16>::value(chunk, e), first + e);
+        for (int e = 0; e < E; ++e) look_at(Row<BF16>::value(chunk, e), first + e, part);
+        if (sums) add(part);
     }
-    rest = sums ? block_sum<THREADS>(rest, sh.red) : 0.0;
-    __syncthreads();
+    if (sums) rest = (double)block_reduce<u64, THREADS>(units, sh.wave_sum, [](u64 a, u64 b) { return a + b; }) * __builtin_ldexp(1.0, power - 41);
+    else __syncthreads();
     Found f;
     f.count = (int)uniform((uint32_t)sh.count);
     f.whole = bound == kLow;
@@ -1095,7 +1108,7 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     f.top = largest_logit;
     f.rest = rest * exp2_neg(-by_T.drift(), 0);
     f.ok = f.count <= kList && queued <= kQueue;
-    f.summed = rest < 1e30 && by_T.sound() && f.top < __builtin_huge_valf();
+    f.summed = !uniform((uint32_t)sh.beyond) && rest < 1e30 && by_T.sound() && f.top < __builtin_huge_valf();
     return f;
 }
 
@@ -1318,13 +1331,14 @@ template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(T
     }
     bool reaches = !done && f.ok && (!sums || f.summed) && (!par.k || f.count >= par.k || f.whole);
     if (reaches && sums && !f.whole) {
-        // (what the list weighs, nearly: a list that cannot reach is not put in order)
-        const Exp<BF16> by_T(par.T, f.ref);
-        double part = 0.0;
-        for (int e = threadIdx.x; e < f.count; e += THREADS) part += (double)by_T(value_in(sh.listed[e]));
-        part = block_sum<THREADS>(part, sh.red);
+        // (what the list weighs, nearly, in whole units again: a list that cannot reach is not put in order)
+        const Exp<BF16> by_T(par.T, f.top);
+        u64 units = 0;
+        for (int e = threadIdx.x; e < f.count; e += THREADS) units += (u64)(by_T(value_in(sh.listed[e])) * 0x1p40f);
+        const double part = (double)block_reduce<u64, THREADS>(units, sh.wave_sum, [](u64 a, u64 b) { return a + b; }) * 0x1p-40;
+        const double beside = f.rest * (double)by_T(f.ref);
         const float share = par.top_p < 1.0f ? par.top_p : par.min_p > 0.0f ? 0.0f : u;
-        reaches = part * 1.001 >= (double)share * (part + f.rest);
+        reaches = part * 1.001 >= (double)share * (part + beside);
     }
     if (reaches && sort_list<THREADS>(sh, f.count)) {
         const float m = value_in(sh.listed[0]);
