@@ -170,6 +170,29 @@ __device__ __forceinline__ Teacher read_record(const Record &rec, const DistillA
         p_sum += q;
         rec.p[j] = q;
     }
+    // Places named twice: the lowest entry stands for them, whichever thread came first to the bitmap
+    if (__any(twice)) {
+        wave_sync();
+        in = in_ce = 0.0;
+        for (int j = lane; j < p.k; j += kWave) {
+            rec.t[j] = 0.f;  // (the record's t is not needed any more)
+            rec.first[j] = false;
+            int l = 0;
+            while (rec.at[l] != rec.at[j]) ++l;
+            if (rec.at[j] < 0 || l < j) continue;
+            rec.first[j] = true;
+            double q = 0.0;
+            for (; l < p.k; ++l)
+                if (rec.at[l] == rec.at[j]) q += rec.p[l];
+            rec.t[j] = (float)q;
+            if (sums) {
+                in += (double)by_tau(rec.z[j]);
+                if (two) in_ce += (double)plain(rec.z[j]);
+            }
+        }
+        wave_sync();
+        for (int j = lane; j < p.k; j += kWave) rec.p[j] = (double)rec.t[j];
+    }
     out.p_sum = wave_sum(p_sum);
     out.r = p.t_lse ? fmax(0.0, 1.0 - out.p_sum) : 0.0;
     if (sums) {
@@ -177,18 +200,6 @@ __device__ __forceinline__ Teacher read_record(const Record &rec, const DistillA
         out.cross = wave_sum(cross);
         out.in = wave_sum(in);
         out.in_ce = two ? wave_sum(in_ce) : out.in;
-    }
-    if (__any(twice)) {
-        wave_sync();
-        for (int j = lane; j < p.k; j += kWave) {
-            double q = 0.0;
-            if (rec.first[j])
-                for (int l = 0; l < p.k; ++l)
-                    if (rec.at[l] == rec.at[j]) q += rec.p[l];
-            rec.t[j] = (float)q;  // (the record's t is not needed any more)
-        }
-        wave_sync();
-        for (int j = lane; j < p.k; j += kWave) rec.p[j] = (double)rec.t[j];
     }
     return out;
 }
