@@ -515,7 +515,7 @@ int collm_sample(int device, const collm_logits *shape, const void *logits, cons
  *   values       dev fp32 [n_rows, k];  indices: dev int32 [n_rows, k].  Where a row has fewer than k logits above -inf:
  *                -inf and index -1 behind them.  NaN counts as -inf here.
  *   lse          dev fp32 [n_rows] or NULL; over all logits of the row (a NaN among them: NaN; otherwise with +inf: +inf)
- * 1 <= k <= COLLM_MAX_TOP; temperature > 0 and finite.
+ * 1 <= k <= COLLM_MAX_TOP; temperature finite and at least 2^-127 (of which 1 / temperature is a number of 32 bits).
  */
 int collm_top_logits(int device, const collm_logits *shape, const void *logits, int32_t k, float temperature, float *values, int32_t *indices,
                      float *lse, void *workspace, int64_t workspace_bytes, void *stream);
@@ -543,7 +543,7 @@ int collm_top_logits(int device, const collm_logits *shape, const void *logits, 
  *   dlogits      dev, element type `dtype`, rows as those of the logits with ld_grad elements from one to the next; only the call's
  *                rows are written.  Either apart from the logits or in their place (same pointer, ld_grad == ld).
  * Sums are kept in 32 bits within a thread and in 64 across threads; a gradient is rounded once.
- * 1 <= k <= COLLM_MAX_TOP; temperature > 0; weights finite.  collm_distill_fwd_bwd is both calls in one that reads the logits once.
+ * 1 <= k <= COLLM_MAX_TOP; temperature as there; weights finite.  collm_distill_fwd_bwd is both calls in one that reads the logits once.
  */
 typedef struct {
     int32_t k;

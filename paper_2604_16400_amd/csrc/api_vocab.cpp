@@ -14,6 +14,8 @@ namespace {
 inline bool aligned(const void *p, unsigned n) { return ((uintptr_t)p & (n - 1)) == 0; }
 inline int elem_bytes(const collm_logits *s) { return s->dtype == COLLM_BF16 ? 2 : 4; }
 
+inline bool temperature_ok(float t) { return t >= kLeastTemperature && std::isfinite(t); }
+
 // Everything that a call's rows can be refused for.  COLLM_OK with s->n_rows == 0: nothing to do.
 int check_rows(const collm_logits *s, const void *logits, LogitRows &r)
 {
@@ -47,7 +49,7 @@ int check_distill(const collm_logits *s, const void *logits, const collm_distill
     const int rc = check_rows(s, logits, a.r);
     if (rc != COLLM_OK) return rc;
     if (!d) return COLLM_E_NULL;
-    if (d->k < 1 || d->k > kMaxTop || !(d->temperature > 0.0f) || !std::isfinite(d->temperature)) return COLLM_E_SHAPE;
+    if (d->k < 1 || d->k > kMaxTop || !temperature_ok(d->temperature)) return COLLM_E_SHAPE;
     if (!std::isfinite(d->kd_weight) || !std::isfinite(d->ce_weight)) return COLLM_E_SHAPE;
     if (s->n_rows == 0) return COLLM_OK;
     if (!d->values || !d->indices) return COLLM_E_NULL;
@@ -126,7 +128,7 @@ int collm_top_logits(int device, const collm_logits *shape, const void *logits, 
     int rc = check_rows(shape, logits, a.r);
     if (rc == COLLM_OK) rc = check_workspace(workspace, workspace_bytes);
     if (rc != COLLM_OK) return rc;
-    if (k < 1 || k > kMaxTop || !(temperature > 0.0f) || !std::isfinite(temperature)) return COLLM_E_SHAPE;
+    if (k < 1 || k > kMaxTop || !temperature_ok(temperature)) return COLLM_E_SHAPE;
     if (shape->n_rows == 0) return COLLM_OK;
     if (!values || !indices) return COLLM_E_NULL;
     if (!aligned(values, 4) || !aligned(indices, 4) || !aligned(lse, 4)) return COLLM_E_ALIGN;

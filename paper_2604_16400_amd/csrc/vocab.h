@@ -9,6 +9,7 @@ namespace collm {
 constexpr int kMaxVocab = 1 << 20;  // columns of a row of logits (a bitmap of a row fits the LDS; fixed-point sums have 20 bits to grow)
 constexpr int kMaxTop = 1024;       // entries of a teacher's record
 constexpr int kDistillStats = 8;    // floats that a forward call keeps of a row for the backward call
+constexpr float kLeastTemperature = 0x1p-127f;  // of a call: log2(e) over it is a number of 32 bits
 constexpr int kLaunchRows = 1 << 21;  // rows of one launch at most: a block of up to 1024 threads each, and a grid has fewer than 2^32
 static_assert((int64_t)kLaunchRows * 1024 < (int64_t)1 << 32, "threads of a grid");
 
