@@ -1301,11 +1301,11 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
     }
 }
 
-// One block a row; SLOTS > 0: alone on its compute unit (of bf16 it holds that many chunks a thread).  What bounds it: one pass over the row, and
+// One block a row.  ALONE: with a compute unit's registers to itself; SLOTS: chunks of a row of bf16 that a thread then holds.  What bounds it: one pass over the row, and
 // the latency of the steps behind it; by value, the counters (2 to 3 logits a cycle and compute unit); by steps, the 64-bit weights (30 instructions a
 // logit).  Measured: 1024 x 128256 bf16 with top-k 20 54 us (4.9 TB/s), with top-p 0.9 102 (by value); 256 rows of them mixed 31; 200 x 50257 fp32 with top-p
 // 0.5 23 us (off the list), 0.9 50 (by steps); one row of 32000 bf16 8.3 greedy, 12.3 with top-k 50 and top-p, 14.3 with top-p alone.
-template <bool BF16, int THREADS, int SLOTS> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) sample_kernel(SampleArgs p)
+template <bool BF16, int THREADS, bool ALONE, int SLOTS> __global__ void __launch_bounds__(THREADS, ALONE ? 4 : 8) sample_kernel(SampleArgs p)
 {
     __shared__ Shared<THREADS> sh;
     const int i = blockIdx.x, wave = (int)uniform((uint32_t)threadIdx.x / kWave);
@@ -1461,11 +1461,11 @@ hipError_t launch_sample(const SampleArgs &a, hipStream_t st)
     // steps 57.6 -> 54.8.  More rows go two to a compute unit: 1024 of 128256 with top-k 54 us, 73 with one.
     const int chunks = a.r.vocab / 8;
     const bool alone = a.r.n_rows <= a.compute_units;
-    if (!a.r.bf16 && alone) COLLM_LAUNCH((sample_kernel<false, 1024, 4>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
-    else if (!a.r.bf16) COLLM_LAUNCH((sample_kernel<false, 1024, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
-    else if (alone && chunks <= 4 * 1024) COLLM_LAUNCH((sample_kernel<true, 1024, 4>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
-    else if (alone && chunks <= 16 * 1024) COLLM_LAUNCH((sample_kernel<true, 1024, 16>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
-    else COLLM_LAUNCH((sample_kernel<true, 1024, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    if (!a.r.bf16 && alone) COLLM_LAUNCH((sample_kernel<false, 1024, true, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    else if (!a.r.bf16) COLLM_LAUNCH((sample_kernel<false, 1024, false, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    else if (alone && chunks <= 4 * 1024) COLLM_LAUNCH((sample_kernel<true, 1024, true, 4>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    else if (alone && chunks <= 16 * 1024) COLLM_LAUNCH((sample_kernel<true, 1024, true, 16>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
+    else COLLM_LAUNCH((sample_kernel<true, 1024, false, 0>), dim3(a.r.n_rows), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 
