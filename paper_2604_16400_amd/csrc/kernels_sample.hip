@@ -1108,7 +1108,9 @@ template <bool BF16, int THREADS> __device__ __forceinline__ Found list_row(Shar
     f.top = largest_logit;
     f.rest = rest * exp2_neg(-by_T.drift(), 0);
     f.ok = f.count <= kList && queued <= kQueue;
-    f.summed = !uniform((uint32_t)sh.beyond) && rest < 1e30 && by_T.sound() && f.top < __builtin_huge_valf();
+    // (A term's exponent t is off by 3 2^-24 of itself at most, and terms so small that this matters are less than half a unit of the weights: up to t = 32, where
+    // the sum is less than 2^64, the error stays below 5e-6 of it.)
+    f.summed = !uniform((uint32_t)sh.beyond) && rest < 0x1p64 && by_T.sound() && f.top < __builtin_huge_valf();
     return f;
 }
 

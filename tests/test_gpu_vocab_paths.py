@@ -75,3 +75,21 @@ def test_every_way_gives_the_same_token(V, temperature, top_p, min_p):
     want = _tokens(z, u, temperature, top_p, min_p, "bf16")
     assert _tokens(z, u, temperature, top_p, min_p, "f32") == want
     assert _tokens(nan, u, temperature, top_p, min_p, "f32") == want
+
+
+@pytest.mark.parametrize("rise", [5.0, 21.0, 23.0, 40.0, 60.0, 90.0])
+def test_rows_that_rise_behind_their_beginning(rise):
+    """What the listing pass's sum is relative to lies far below the rest of the row: at some distance the row goes by steps."""
+    V = 50257
+    rng = np.random.default_rng(int(rise))
+    z = np.repeat((rng.normal(size=(2, V)) * np.array([0.001, 1.0])[:, None]).astype(np.float32), 60, axis=0)
+    z[:, 16400:] += np.float32(rise)
+    z[:, 30000] = rise + 9.0
+    z[:, V - 1] = -INF
+    nan = z.copy()
+    nan[:, V - 1] = NAN
+    u = rng.random(len(z)).astype(np.float32)
+    for top_p, min_p in ((1.0, 0.0), (0.1, 0.0), (0.9, 0.0), (1.0, 0.5)):
+        want = [ov.sample_whole(row, x, 1.0, 0, top_p, min_p)[0] for row, x in zip(z, u)]
+        assert _tokens(nan, u, 1.0, top_p, min_p, "f32") == want
+        assert _tokens(z, u, 1.0, top_p, min_p, "f32") == want
