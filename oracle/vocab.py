@@ -106,7 +106,10 @@ def distill(z, t, at, t_lse=None, label=-1, temperature=1.0, kd_weight=1.0, ce_w
         kd = sum(x * (np.log(x) - (z[v] / tau - lse)) for x, v in zip(p, at) if x > 0)
         teacher = np.zeros(V)
         np.add.at(teacher, at, p)
-        rest = np.where(outside, np.exp(z / tau - (lse_out if lse_out > -np.inf else 0.0)), 0.0)
+        rest = np.zeros(V)
+        if lse_out > -np.inf:  # (from the rest's largest: beside 1e38 the logarithm of their number would be lost)
+            rest[outside] = np.exp((z[outside] - z[outside].max()) / tau)
+            rest /= rest.sum()
         if r > 0:
             kd += r * (np.log(r) - (lse_out - lse))
         P = p.sum() + r
