@@ -500,7 +500,8 @@ typedef struct {
  *   params       the rows' parameters, each dev [n_rows] or NULL (temperature 1, the others off); or NULL
  *   u            dev fp32 [n_rows], each in [0, 1)
  *   token        dev int32 [n_rows]; -1 where every logit is -inf
- *   logprob      dev fp32 [n_rows] or NULL: logarithm of the probability, among the kept, of the token (-inf beside token -1)
+ *   logprob      dev fp32 [n_rows] or NULL: logarithm of the probability, among the kept, of the token (-inf beside token -1); where nothing cuts a
+ *                row it may be off by up to 5e-6 (the sum of the row is then taken in 32 bits)
  */
 typedef struct {
     const float *temperature;
@@ -542,7 +543,7 @@ int collm_top_logits(int device, const collm_logits *shape, const void *logits, 
  *   dloss        dev fp32 [n_rows]
  *   dlogits      dev, element type `dtype`, rows as those of the logits with ld_grad elements from one to the next; only the call's
  *                rows are written.  Either apart from the logits or in their place (same pointer, ld_grad == ld).
- * Sums are kept in 32 bits within a thread and in 64 across threads; a gradient is rounded once.
+ * The exponentials of 16 bytes of a row are added in 32 bits and all else in 64; a gradient is rounded once.
  * 1 <= k <= COLLM_MAX_TOP; temperature as there; weights finite.  collm_distill_fwd_bwd is both calls in one that reads the logits once.
  */
 typedef struct {

@@ -467,8 +467,10 @@ template <bool BF16> __device__ __forceinline__ void mask_chunk(uint4 &v, const 
 
 // A block takes rows blockIdx.x, + gridDim.x, ..: record, sums, loss, and with GRAD the gradient.  While a row's gradient is written, each
 // chunk's registers take the next row's: the memory has work while the block computes, though a row of 128 Ki bf16
-// leaves no registers for a second block beside it.  Bound by memory: loss and gradient of 8192 x 128256 bf16 996 us (4.2 TB/s), loss alone of 1792 x 32000 bf16
-// 25.9 us (4.4 TB/s); 32 x 32000 in one call 11.4 us.  The first wave does the record's and the row's arithmetic in 64 bits.
+// leaves no registers for a second block beside it.  With 16 or 20 chunks a thread also has 160 to 260 bytes of scratch memory: addresses and constants that
+// are read again between the sums and the gradient, not the row (3 % more bytes written than the gradient has).  Bound by memory: loss and gradient of 8192 x 128256
+// bf16 975 us (4.3 TB/s), of 1000 x 128256 fp32 268 (3.8 TB/s), loss alone of 1792 x 32000 bf16 25 us (4.6 TB/s), of 1000 x 128256 fp32 82 (6.3 TB/s, in part from
+// the last-level cache); 32 x 32000 in one call 11.3 us.  The first wave does the record's and the row's arithmetic in 64 bits.
 template <bool BF16, int THREADS, int SLOTS, bool GRAD, bool ONCE> __global__ void __launch_bounds__(THREADS, SLOTS ? 4 : 8) distill_kernel(DistillArgs p)
 {
     constexpr int E = Row<BF16>::E, W = THREADS / kWave;

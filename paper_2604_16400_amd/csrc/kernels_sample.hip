@@ -7,8 +7,8 @@
 // One pass over the row lists its beginning and adds up the rest: a logit is listed if it is not below a bound which at least
 // `want` logits reach, taken from the threads' largest logits so far (the least, over the waves, of the (want / waves)-th largest of
 // a wave's 64).  The list, a few times `want`, is put in order by a counting sort over equal steps of the logit, and all
-// that is asked is read off it in 64 bits.  The sum of the rest need only be near: where its error could change what comes out, and where the
-// list does not reach far enough, the row is done by steps instead: exact for every row, in more passes.
+// that is asked is read off it in 64 bits.  The sum of the rest need only be near: where its error, with the rounding of every weight in it, could change
+// what comes out, and where the list does not reach far enough, the row is done by steps instead: exact for every row, in more passes.
 //
 // Rows of bf16 that are cut by their weights are not listed: they have few different logits.  One pass counts each (of either sign those of
 // 32 octaves, 2^-15 to 2^17; what lies nearer to 0 is listed), a weight is computed once for each that occurs, and a running sum
@@ -1304,9 +1304,11 @@ __device__ __forceinline__ void read_list(Shared<THREADS> &sh, const Params &par
 }
 
 // One block a row.  ALONE: with a compute unit's registers to itself; SLOTS: chunks of a row of bf16 that a thread then holds.  What bounds it: one pass over the row, and
-// the latency of the steps behind it; by value, the counters (2 to 3 logits a cycle and compute unit); by steps, the 64-bit weights (30 instructions a
-// logit).  Measured: 1024 x 128256 bf16 with top-k 20 54 us (4.9 TB/s), with top-p 0.9 102 (by value); 256 rows of them mixed 31; 200 x 50257 fp32 with top-p
-// 0.5 23 us (off the list), 0.9 50 (by steps); one row of 32000 bf16 8.3 greedy, 12.3 with top-k 50 and top-p, 14.3 with top-p alone.
+// the latency of the steps behind it; by value, the counters (2.1 logits a cycle and compute unit; shared memory is at work 34 % of the cycles, half of that
+// bank conflicts, the vector units 41 %) and a second reading of 0.85 of the row (rounds of 32768 logits, one ahead, up to the drawn one); by steps, 87 vector
+// instructions a logit in three passes, 30 of them the listing's and most others the 64-bit weights' (half of the cycles).  Measured: 1024 x 128256 bf16 with top-k 20 55 us (4.8 TB/s),
+// with top-p 0.9 102 (by value); 256 rows of them mixed 31; 200 x 50257 fp32 with top-p 0.5 23.5 us (off the list), 0.9 50 (by steps); one row of 32000 bf16 8.6
+// greedy, 12.6 with top-k 50 and top-p, 14.5 with top-p alone.
 template <bool BF16, int THREADS, bool ALONE, int SLOTS> __global__ void __launch_bounds__(THREADS, ALONE ? 4 : 8) sample_kernel(SampleArgs p)
 {
     __shared__ Shared<THREADS> sh;
@@ -1369,8 +1371,9 @@ template <bool BF16, int THREADS, bool ALONE, int SLOTS> __global__ void __launc
     }
 }
 
-// One block a row, two to a compute unit.  Bound by memory where there are many rows: 3277 x 128256 bf16, k 64, 179 us (4.7 TB/s); 205 x 50257 bf16, k 250,
-// 18 us; 32 x 32000 fp32, k 20, 12.3 us (one pass and a dozen block-wide waits).  A list that is too long: by steps, the k-th place by counting, then the k logits up to it.
+// One block a row, two to a compute unit.  Bound by memory where there are many rows: 3277 x 128256 bf16, k 64, 180 us (4.7 TB/s), 1000 x 128256
+// fp32 97 (5.3 TB/s); 205 x 50257 bf16, k 250, 17.5 us; 32 x 32000 fp32, k 20, 12.7 us (one pass and a dozen block-wide waits).  A list that is too long, and k above 256:
+// by steps, the k-th place by counting, then the k logits up to it (205 x 50257 bf16, k 300 / 1024, 50 / 68 us).
 template <bool BF16, int THREADS> __global__ void __launch_bounds__(THREADS, 8) top_kernel(TopArgs p)
 {
     __shared__ Shared<THREADS> sh;
