@@ -466,7 +466,7 @@ int collm_adapter_adamw(int device, collm_dtype dtype, void *param, float *maste
  * same bits on every run.
  *
  *   logits       dev, element type `dtype`: row r is the `vocab` elements from r * ld on (ld >= vocab), n_held rows in all;
- *                element-aligned, as is every other pointer of these calls but `workspace`
+ *                element-aligned, as is every other pointer of these calls but `workspace`; may be NULL if n_held == 0
  *   rows         dev int32 [n_rows]: row i of the call is row rows[i] of the logits (the rows of the kind in question among
  *                those of a mixed batch), or NULL: rows 0 .. n_rows - 1 (n_rows <= n_held).  An entry outside
  *                [0, n_held) is a row that is not there: token -1, an empty record, loss 0.  Where gradients are

@@ -25,7 +25,7 @@ int check_rows(const collm_logits *s, const void *logits, LogitRows &r)
     if (!s->rows && s->n_rows > s->n_held) return COLLM_E_SHAPE;
     if (s->n_held > 1 && s->ld > (INT64_MAX / 8) / s->n_held) return COLLM_E_SHAPE;
     if (s->n_rows == 0) return COLLM_OK;
-    if (!logits) return COLLM_E_NULL;
+    if (!logits && s->n_held > 0) return COLLM_E_NULL;  // (of no held row there is no memory: the call's rows are not there)
     if (!aligned(logits, elem_bytes(s)) || !aligned(s->rows, 4)) return COLLM_E_ALIGN;
     r.logits = logits;
     r.ld = s->ld;
@@ -70,7 +70,7 @@ int check_grad(const collm_logits *s, const void *logits, const float *dloss, co
 {
     if (ld_grad < s->vocab || (s->n_held > 1 && ld_grad > (INT64_MAX / 8) / s->n_held)) return COLLM_E_SHAPE;
     if (s->n_rows == 0) return COLLM_OK;
-    if (!dloss || !dlogits) return COLLM_E_NULL;
+    if (!dloss || (!dlogits && s->n_held > 0)) return COLLM_E_NULL;
     if (!aligned(dloss, 4) || !aligned(dlogits, elem_bytes(s))) return COLLM_E_ALIGN;
     if (s->n_held == 0) return COLLM_OK;
     const uintptr_t z = (uintptr_t)logits, g = (uintptr_t)dlogits;
